@@ -1,0 +1,530 @@
+"""Operators of language models, proven layer by layer over F_p, p = 2^61 - 1:
+
+  embed  a token embedding with scaling as a layer: C = scale E[token] (a
+         row of zeros for token -1), rounded to s fewer bits, with its proof
+         (ra.prove_embed);
+  gate   the product of a gated feed-forward block as a layer: C = A * B entry
+         by entry, rounded, with its proof (ra.prove_gate);
+  ffn    the whole block: both projections (ReLU on the gate's), the gated
+         product and the projection back (ra.prove_gated_ffn).
+
+A pass is one request: the layer's integer tables (C, the rounded output R,
+its remainder Rm, Y = |R|, the output Z, the packed bit table) and the
+transcript of its sum-checks.  Every output is an integer or a field element
+and is the same in any correct implementation.  The verifier's challenges
+come from a seeded stream (xorshift64 with shifts 13, 7, 17, each output mod
+p) that goes on from pass to pass, so no two passes answer the same question.
+
+A layer consumes, in order: r1 (log n), r2 (log k), the rounds of its product
+(embed: log2 of the vocabulary, rounded up; gate: log n k; a projection: log
+m), lambda1..3, mu, tau (log P), sigma (log P + log n k) and with ReLU rho'
+(log n k).
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+DEV = "cuda"
+P = (1 << 61) - 1
+M31 = (1 << 31) - 1
+TABLES = ("C", "R", "Rm", "Y", "Z", "bits")
+
+
+# --- cases -------------------------------------------------------------------
+def _embed(name, n, vocab, d, t=16, mode=0):
+    c = dict(op="embed", n=n, vocab=vocab, d=d, s=8, t=t, mode=mode)
+    return dict(name=name, **c) if name else c
+
+
+def _gate(name, n, k, s, bits, t, mode=0):
+    c = dict(op="gate", n=n, k=k, s=s, bits=bits, t=t, mode=mode)
+    return dict(name=name, **c) if name else c
+
+
+def _ffn(name, n, d, hidden, t=12, relu=True):
+    c = dict(op="ffn", n=n, d=d, hidden=hidden, s=8, t=t, relu=relu)
+    return dict(name=name, **c) if name else c
+
+
+def listed():
+    return [
+        # one token of a small vocabulary: the smallest call, its latency
+        _embed("embed-token", 1, 4000, 256),
+        # a ragged prompt, odd vocabulary and width, t from the data
+        _embed("embed-ragged", 100, 5003, 300, t=-1),
+        # a prompt through a usual table
+        _embed("embed-prompt", 512, 32000, 2048),
+        # one token against a large table: the table's pass is all there is
+        _embed("embed-token-large", 1, 128000, 4096),
+        # a long prompt against a large table
+        _embed("embed-large", 1024, 128000, 4096),
+        # one token's gated product: the smallest call
+        _gate("gate-token", 1, 4096, 8, 12, 15),
+        # a ragged batch and width, literal floor rounding, t from the data
+        _gate("gate-ragged", 37, 2730, 8, 12, -1, mode=1),
+        # a batch of tokens
+        _gate("gate-batch", 256, 4096, 8, 12, 15),
+        # a prompt through a wide block, larger values
+        _gate("gate-large", 512, 11008, 12, 15, 17),
+        # one token through a whole block
+        _ffn("ffn-token", 1, 1024, 2730),
+        # a small block, a batch of tokens, t from the data
+        _ffn("ffn-small", 64, 256, 683, t=-1),
+        # a prompt through a block
+        _ffn("ffn-large", 512, 2048, 5461),
+    ]
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, round(math.exp(rng.uniform(math.log(lo), math.log(hi))))))
+
+
+def draw(rng):
+    op = rng.choice(["embed", "gate", "ffn"])
+    mode = int(rng.random() < 0.25)
+    if op == "embed":
+        return _embed("", _log(rng, 1, 1024), _log(rng, 1000, 128000), _log(rng, 64, 4096),
+                      rng.choice([16, 16, -1]), mode)
+    if op == "gate":
+        n = _log(rng, 1, 512)
+        return _gate("", n, _log(rng, 64, 11008), *rng.choice([(8, 12, 15), (8, 12, -1), (12, 15, 17)]), mode)
+    return _ffn("", _log(rng, 1, 512), _log(rng, 64, 2048), _log(rng, 128, 5461), rng.choice([12, 12, -1]),
+                rng.random() < 0.75)
+
+
+# --- inputs ------------------------------------------------------------------
+def _pow2(x):
+    return 1 << max(0, (int(x) - 1).bit_length())
+
+
+def _seed64(seed):
+    return (0x9E3779B97F4A7C15 * (2 * int(seed) + 1)) & 0xFFFFFFFFFFFFFFFF or 1
+
+
+def _normal(g, rows, cols, std, top, dtype, lo=None):
+    """rows x cols of N(0, std^2), rounded and clamped to [lo, top], padded with zeros to powers of two."""
+    x = torch.randn((rows, cols), generator=g, device=DEV) * std
+    out = torch.zeros((_pow2(rows), _pow2(cols)), dtype=dtype, device=DEV)
+    out[:rows, :cols] = x.round().clamp(-top if lo is None else lo, top).to(dtype)
+    return out
+
+
+def _inputs(case, seed):
+    g = torch.Generator(device=DEV).manual_seed(int(seed) & 0x7FFFFFFFFFFFFFFF)
+    one = 1 << case["s"]
+    if case["op"] == "embed":
+        # tokens as in text: a few are in every other place, most are rare
+        n, vocab = case["n"], case["vocab"]
+        u = torch.rand(n, generator=g, device=DEV, dtype=torch.float64)
+        tok = torch.full((_pow2(n),), -1, dtype=torch.int32, device=DEV)
+        tok[:n] = (torch.exp(u * math.log(vocab + 1)) - 1).to(torch.int32).clamp(0, vocab - 1)
+        E = (torch.randn((vocab, case["d"]), generator=g, device=DEV) * one).round().clamp(-8 * one, 8 * one)
+        return dict(tok=tok, E=E.to(torch.int16), scale=round(math.sqrt(case["d"]) * one))
+    if case["op"] == "gate":
+        top = (1 << case["bits"]) - 1
+        return dict(A=_normal(g, case["n"], case["k"], top / 4, top, torch.int32, lo=0),
+                    B=_normal(g, case["n"], case["k"], top / 4, top, torch.int32))
+    n, d, h = case["n"], case["d"], case["hidden"]
+    return dict(X=_normal(g, n, d, one / 2, 4 * one, torch.int16),
+                Wg=_normal(g, d, h, 4 * one / math.sqrt(d), 32 * one, torch.int16),
+                Wu=_normal(g, d, h, 4 * one / math.sqrt(d), 32 * one, torch.int16),
+                Wd=_normal(g, h, d, one / math.sqrt(h), 8 * one, torch.int16))
+
+
+def _n_layers(case):
+    return 4 if case["op"] == "ffn" else 1
+
+
+def prepare(case, seed):
+    st = dict(case=dict(case), x=_seed64(seed), **_inputs(case, seed))
+    if own:  # the prover's context and the outputs' buffers, as a server keeps them
+        from paper_2505_17623_amd import ra
+        st["ra"], st["bufs"] = ra, [{} for _ in range(_n_layers(case))]
+        ctx = ra.Context(seed=1, deferred=case["t"] >= 0)
+        _own(ctx, st)
+        ctx.close()
+        st["ctx"] = ra.Context(seed=_seed64(seed), deferred=case["t"] >= 0)
+    return st
+
+
+# --- the framework's operators -----------------------------------------------
+SCALARS = ("r_claim", "rm_claim", "y_claim", "z_claim", "range_sum", "bits_claim", "r_at", "y_at", "t", "P")
+
+
+def _own(ctx, st):
+    ra, c, bufs = st["ra"], st["case"], st["bufs"]
+    if c["op"] == "embed":
+        res = [ra.prove_embed(ctx, st["tok"], st["E"], st["scale"], c["s"], mode=c["mode"], t=c["t"], bufs=bufs[0])]
+    elif c["op"] == "gate":
+        res = [ra.prove_gate(ctx, st["A"], st["B"], c["s"], mode=c["mode"], t=c["t"], bufs=bufs[0])]
+    else:
+        res = ra.prove_gated_ffn(ctx, st["X"], st["Wg"], st["Wu"], c["s"], Wd=st["Wd"], gate_relu=c["relu"],
+                                 ts=None if c["t"] < 0 else [c["t"]] * 4, bufs=bufs)
+    if ctx.deferred:
+        ctx.sync()  # the proof is written out
+    out = []
+    for r in res:
+        tr = r["transcript"]
+        gate = "gate_evals" in tr
+        words = tr["gate_evals" if gate else "mm_evals"] + tr["rs_evals"] + tr["zc_evals"]
+        words = words + [tr["c0"], tr["a_at" if gate else "a_star"], tr["b_at" if gate else "b_star"]]
+        out.append({**{k: r[k].reshape(-1) for k in TABLES},
+                    "transcript": np.array(words + [tr[k] for k in SCALARS], dtype=np.int64)})
+    return out
+
+
+# --- the plain form: arithmetic mod p in int64 tensors -----------------------
+def _fold(x):
+    x = (x & P) + (x >> 61)
+    return torch.where(x >= P, x - P, x)
+
+
+def _mul(a, b):
+    """a b mod p for a, b in [0, p) (b may be an int): 31-bit halves, 2^61 = 1."""
+    a0, a1, b0, b1 = a & M31, a >> 31, b & M31, b >> 31
+    mid, lo = a1 * b0 + a0 * b1, a0 * b0
+    return _fold(2 * (a1 * b1) + (mid >> 30) + ((mid & ((1 << 30) - 1)) << 31) + (lo & P) + (lo >> 61))
+
+
+def _add(a, b):
+    return _fold(a + b)
+
+
+def _sub(a, b):
+    return _fold(a + (P - b))
+
+
+def _sum(x):
+    """The sum mod p of a table of at most 2^31 entries."""
+    return _add(_mul((x >> 31).sum() % P, 1 << 31), (x & M31).sum() % P)
+
+
+def _eq(point):
+    """eq(point, i) for every i, the first coordinate the most significant bit (Eq. (1))."""
+    T = torch.ones(1, dtype=torch.int64, device=DEV)
+    for z in point:
+        hi = _mul(T, z)
+        T = torch.stack([_sub(T, hi), hi], -1).reshape(-1)
+    return T
+
+
+def _dot(M, e):
+    """M e mod p for a matrix of integers below 2^20 and field elements e (at
+    most 2^12): e in 21-bit limbs, products in float64 that stay below 2^53."""
+    limbs = torch.stack([e & 0x1FFFFF, (e >> 21) & 0x1FFFFF, e >> 42], 1).double()
+    s = (M.double() @ limbs).long() % P
+    return _add(_add(s[:, 0], _mul(s[:, 1], 1 << 21)), _mul(s[:, 2], 1 << 42))
+
+
+def _rounds(tables, f, degree, point):
+    """The sum-check (Sec. II-D) of sum_i f(tables at i): the round
+    polynomials' values at 0 .. degree and the tables' final values."""
+    evals = []
+    for r in point:
+        lo, hi = zip(*[T.chunk(2) for T in tables])
+        step, at = [_sub(h, l) for l, h in zip(lo, hi)], list(lo)
+        for X in range(degree + 1):
+            evals.append(_sum(f(*at)))
+            at = [_add(a, d) for a, d in zip(at, step)]
+        tables = [_add(l, _mul(d, r)) for l, d in zip(lo, step)]
+    return evals, [T[0] for T in tables]
+
+
+def _draws(st, count):
+    x, out = st["x"], []
+    for _ in range(count):
+        x ^= (x << 13) & 0xFFFFFFFFFFFFFFFF
+        x ^= x >> 7
+        x ^= (x << 17) & 0xFFFFFFFFFFFFFFFF
+        out.append(x % P)
+    st["x"] = x
+    return out
+
+
+def _lg(x):
+    return _pow2(x).bit_length() - 1
+
+
+def _witness(C, s, t, mode, relu):
+    cc = C + (0 if mode else 1 << (s - 1))
+    R = cc >> s
+    if t < 0:  # the least t with R in [-2^(t+1), 2^(t+1))
+        t = max(int(torch.where(R >= 0, R, -R - 1).max()).bit_length() - 1, 0)
+    Rm, Y = cc & ((1 << s) - 1), R.abs()
+    Z = (R + Y) >> 1 if relu else R
+    bits = Rm | ((R + (1 << (t + 1))) << s)
+    used = s + t + 2
+    if relu:
+        bits, used = bits | (Y << used), used + t + 2
+    return R, Rm, Y, Z, bits, t, _pow2(used)
+
+
+def _layer(st, C, product, n, k, s, t, mode, relu):
+    """The layer whose exact product is C (n k entries): product(r1, r2) gives
+    its own sum-check; then the range sum-check over the bit table and with
+    ReLU the zero-check of R^2 = Y^2."""
+    ln, lk = _lg(n), _lg(k)
+    r = _draws(st, ln + lk)
+    ev, c0, fa, fb = product(r[:ln], r[ln:])
+    R, Rm, Y, Z, bits, t, planes = _witness(C, s, t, mode, relu)
+    E = _eq(r)
+    claims = [_sum(_mul(E, T % P)) for T in (R, Rm, Y, Z)]
+    lP = _lg(planes)
+    lam, tau, sigma = _draws(st, 4), _draws(st, lP), _draws(st, lP + ln + lk)
+    groups = [(lam[0], s), (lam[1], t + 2)] + ([(lam[2], t + 2)] if relu else [])
+    W = [lam[3] * g * (1 << b) % P for g, count in groups for b in range(count)]
+    W = torch.tensor(W + [0] * (planes - len(W)), dtype=torch.int64, device=DEV)
+    q = torch.arange(planes, device=DEV)[:, None]
+    b = (bits[None, :] >> q) & 1
+    start = _add(_mul(claims[1], lam[0]), _mul(_add(claims[0], 1 << (t + 1)), lam[1]))
+    if relu:
+        start = _add(start, _mul(claims[2], lam[2]))
+    both = [_mul(w[:, None], E[None, :]).reshape(-1) for w in (_eq(tau), W)]
+    rs, fin = _rounds([b.reshape(-1), *both], lambda b, e, w: _mul(_add(_mul(e, _sub(b, torch.ones_like(b))), w), b),
+                      3, sigma)
+    zero = torch.zeros_like(c0)
+    zc, at = [], [zero, zero, zero]
+    if relu:
+        zc, at = _rounds([E, R % P, Y % P], lambda e, u, v: _mul(e, _sub(_mul(u, u), _mul(v, v))), 3,
+                         _draws(st, ln + lk))
+    words = [*ev, *rs, *zc, c0, fa, fb, *claims, _mul(start, lam[3]), fin[0], at[1], at[2], zero + t, zero + planes]
+    return dict(C=C, R=R.int(), Rm=Rm.short(), Y=Y.int(), Z=Z.int(), bits=bits, transcript=torch.stack(words))
+
+
+def _product2(st, a, b):
+    """The degree-2 sum-check of sum_l a(l) b(l)."""
+    ev, (fa, fb) = _rounds([a, b], _mul, 2, _draws(st, _lg(a.numel())))
+    return ev, _sum(_mul(a, b)), fa, fb
+
+
+def _projection(st, A, B, s, t, mode, relu):
+    C = (A.double() @ B.double()).long().reshape(-1)
+    return _layer(st, C, lambda r1, r2: _product2(st, _dot(A.T, _eq(r1)), _dot(B, _eq(r2))), A.shape[0], B.shape[1],
+                  s, t, mode, relu)
+
+
+def _gated(st, A, B, s, t, mode):
+    n, k = A.shape
+    A, B = A.long().reshape(-1), B.long().reshape(-1)
+
+    def product(r1, r2):
+        ev, (_, fa, fb) = _rounds([_eq(r1 + r2), A % P, B % P], lambda e, a, b: _mul(_mul(e, a), b), 3,
+                                  _draws(st, _lg(n * k)))
+        return ev, _sum(_mul(_mul(_eq(r1 + r2), A % P), B % P)), fa, fb
+    return _layer(st, A * B, product, n, k, s, t, mode, False)
+
+
+def _embedding(st, tok, E, scale, s, t, mode):
+    n, (vocab, d) = tok.numel(), E.shape
+    k, rows = _pow2(d), _pow2(vocab)
+    there = (tok >= 0)[:, None]
+    C = torch.zeros((n, k), dtype=torch.int64, device=DEV)
+    C[:, :d] = torch.where(there, E[tok.clamp(min=0).long()].long() * scale, 0)
+
+    def product(r1, r2):
+        # every token's weight in the sum over its row of the table: sums of 31-bit halves, then mod p
+        w = torch.where(there[:, 0], _mul(_eq(r1), scale % P), 0)
+        at, zeros = tok.clamp(min=0).long(), torch.zeros(rows, dtype=torch.int64, device=DEV)
+        lo, hi = zeros.index_add(0, at, w & M31) % P, zeros.index_add(0, at, w >> 31) % P
+        e = zeros.clone()
+        e[:vocab] = _dot(E, _eq(r2)[:d])
+        return _product2(st, _add(lo, _mul(hi, 1 << 31)), e)
+    return _layer(st, C.reshape(-1), product, n, k, s, t, mode, False)
+
+
+def run(st):
+    if own:
+        return _own(st["ctx"], st)
+    c = st["case"]
+    s, t = c["s"], c["t"]
+    if c["op"] == "embed":
+        return [_embedding(st, st["tok"], st["E"], st["scale"], s, t, c["mode"])]
+    if c["op"] == "gate":
+        return [_gated(st, st["A"], st["B"], s, t, c["mode"])]
+    gate = _projection(st, st["X"], st["Wg"], s, t, 0, c["relu"])
+    up = _projection(st, st["X"], st["Wu"], s, t, 0, False)
+    shape = (st["X"].shape[0], st["Wg"].shape[1])
+    mid = _gated(st, gate["Z"].reshape(shape), up["Z"].reshape(shape), s, t, 0)
+    return [gate, up, mid, _projection(st, mid["Z"].reshape(shape), st["Wd"], s, t, 0, False)]
+
+
+# --- accounting --------------------------------------------------------------
+FIELD_MUL = 8  # operations of a product in F_p: four 32 x 32 -> 64 bit multiply-adds
+
+
+def work(case):
+    """Bytes: operands read once, tables written once (30 an output).
+    Operations: the products, and the sum-checks' field products: 5 a pair of
+    a product instance, 6 and 7 a pair over x of the range and the ReLU
+    instance, one an entry of a binding."""
+    if case["op"] == "embed":
+        n, k, rows = _pow2(case["n"]), _pow2(case["d"]), _pow2(case["vocab"])
+        table = case["vocab"] * case["d"]
+        return {"bytes": 2 * table + 4 * n + 30 * n * k, "flops": FIELD_MUL * (table + 5 * rows + 6 * n * k)}
+    if case["op"] == "gate":
+        N = _pow2(case["n"]) * _pow2(case["k"])
+        return {"bytes": 38 * N, "flops": FIELD_MUL * (7 + 6) * N}
+    n, d, h = (_pow2(case[x]) for x in ("n", "d", "hidden"))
+    by = 2 * n * d + 3 * 2 * d * h + 30 * (3 * n * h + n * d)
+    ops = 3 * 2 * n * d * h + FIELD_MUL * (2 * n * d + 3 * d * h + n * h * (7 * case["relu"] + 6 * 3 + 7) + 6 * n * d)
+    return {"bytes": by, "flops": ops}
+
+
+# --- the definitions in 64 bits, on the host ---------------------------------
+U = np.uint64
+MOST_EXACT = 1 << 21  # entries of a bit table beyond which the transcript would take too long here
+
+
+def _hmul(a, b):
+    """Product mod p of uint64 arrays: four 32-bit partial products, 2^64 = 8."""
+    a, b = np.asarray(a, dtype=U), np.asarray(b, dtype=U)
+    w = U(0xFFFFFFFF)
+    al, ah, bl, bh = a & w, a >> U(32), b & w, b >> U(32)
+    ll, m1, m2, hh = al * bl, ah * bl, al * bh, ah * bh
+    mid = (ll >> U(32)) + m1 + m2  # below 2^62 + 2^32
+    low, high = (ll & w) | (mid << U(32)), hh + (mid >> U(32))
+    x = (low & U(P)) + (low >> U(61)) + (high << U(3))
+    x = (x & U(P)) + (x >> U(61))
+    return np.where(x >= U(P), x - U(P), x)
+
+
+def _hsum(x):
+    return (int((x >> U(32)).sum()) * (1 << 32) + int((x & U(0xFFFFFFFF)).sum())) % P
+
+
+def _hchi(point, v):
+    """The Lagrange basis at `point`, as products over the bits of the index."""
+    i, out = np.arange(1 << v), np.ones(1 << v, dtype=U)
+    for j, z in enumerate(point):
+        bit = (i >> (v - 1 - j)) & 1
+        out = _hmul(out, np.where(bit == 1, U(z), U((1 - z) % P)))
+    return out
+
+
+def _hfield(x):
+    return np.mod(x.astype(np.int64), P).astype(U)
+
+
+def _hmix(lo, hi, X):
+    """(1 - X) lo + X hi mod p."""
+    m = _hmul(lo, U((1 - X) % P)) + _hmul(hi, U(X % P))
+    return np.where(m >= U(P), m - U(P), m)
+
+
+def _hrounds(tables, f, degree, point):
+    ev = []
+    for r in point:
+        h = len(tables[0]) // 2
+        ev += [_hsum(f(*[_hmix(T[:h], T[h:], X) for T in tables])) for X in range(degree + 1)]
+        tables = [_hmix(T[:h], T[h:], r) for T in tables]
+    return ev, [int(T[0]) for T in tables]
+
+
+def _hlayer(st, C, product, n, k, s, t, mode, relu):
+    cc = C + (0 if mode else 1 << (s - 1))
+    R, Rm = np.floor_divide(cc, 1 << s), np.mod(cc, 1 << s)
+    if t < 0:
+        t = 0
+        while R.min() < -(1 << (t + 1)) or R.max() >= 1 << (t + 1):
+            t += 1
+    Y = np.abs(R)
+    Z = np.maximum(R, 0) if relu else R
+    fields = [(Rm, s), (R + (1 << (t + 1)), t + 2)] + ([(Y, t + 2)] if relu else [])
+    planes = _pow2(sum(c for _, c in fields))
+    plane = [((T >> b) & 1) for T, c in fields for b in range(c)]
+    bits = np.zeros(C.size, dtype=np.int64)
+    for q, p in enumerate(plane):
+        bits |= p.astype(np.int64) << q
+    out = dict(C=C, R=R.astype(np.int32), Rm=Rm.astype(np.int16), Y=Y.astype(np.int32), Z=Z.astype(np.int32),
+               bits=bits, transcript=None)
+    ln, lv, lP = _lg(n), _lg(n) + _lg(k), _lg(planes)
+    if planes * C.size > MOST_EXACT:
+        return out
+    r = _draws(st, lv)
+    ev, c0, fa, fb = product(r[:ln], r[ln:])
+    E = _hchi(r, lv)
+    rc, rmc, yc, zc = (_hsum(_hmul(E, _hfield(T))) for T in (R, Rm, Y, Z))
+    l1, l2, l3, mu = _draws(st, 4)
+    tau, sigma = _draws(st, lP), _draws(st, lP + lv)
+    W = [l * (1 << b) % P for l, (_, c) in zip((l1, l2, l3), fields) for b in range(c)]
+    b = np.concatenate(plane + [np.zeros((planes - len(plane)) * C.size, dtype=np.int64)]).astype(U)
+    e = _hmul(_hchi(tau, lP)[:, None], E[None, :]).reshape(-1)
+    w = _hmul(np.array([mu * x % P for x in W] + [0] * (planes - len(W)), dtype=U)[:, None], E[None, :]).reshape(-1)
+
+    def summand(b, e, w):
+        x = _hmul(e, _hmul(b, np.where(b == 0, U(P - 1), b - U(1)))) + _hmul(w, b)
+        return np.where(x >= U(P), x - U(P), x)
+    rs, fin = _hrounds([b, e, w], summand, 3, sigma)
+    total = mu * (l1 * rmc + l2 * (rc + (1 << (t + 1))) + (l3 * yc if relu else 0)) % P
+    ze, at = [], [0, 0, 0]
+    if relu:  # R^2 - Y^2 as (R - Y)(R + Y)
+        z, fz = _hrounds([E, _hfield(R - Y), _hfield(R + Y)], lambda e, u, v: _hmul(_hmul(e, u), v), 3,
+                         _draws(st, lv))
+        half = (P + 1) // 2
+        ze, at = z, [0, (fz[1] + fz[2]) * half % P, (fz[2] - fz[1]) * half % P]
+    words = [*ev, *rs, *ze, c0, fa, fb, rc, rmc, yc, zc, total, fin[0], at[1], at[2], t, planes]
+    out["transcript"] = np.array(words, dtype=np.int64)
+    return out
+
+
+def _hdot(M, e):
+    """M e mod p row by row, entries of M below 2^21 in size: exact int64 sums of 16-bit limbs."""
+    limbs = np.stack([(e >> U(16 * i)) & U(0xFFFF) for i in range(4)], 1).astype(np.float64)
+    s = np.concatenate([M[i:i + 8192].astype(np.float64) @ limbs for i in range(0, M.shape[0], 8192)])
+    total = np.zeros(M.shape[0], dtype=U)
+    for i in range(4):
+        total = (total + _hmul(_hfield(s[:, i]), U(1 << (16 * i)))) % U(P)
+    return total
+
+
+def exact(case, seed):
+    st = dict(x=_seed64(seed))
+    a = {k: v.cpu().numpy() if isinstance(v, torch.Tensor) else v for k, v in _inputs(case, seed).items()}
+    s, t = case["s"], case["t"]
+
+    def product2(u, v):
+        ev, (fu, fv) = _hrounds([u, v], _hmul, 2, _draws(st, _lg(u.size)))
+        return ev, _hsum(_hmul(u, v)), fu, fv
+
+    def projection(A, B, relu):
+        C = (A.astype(np.float64) @ B.astype(np.float64)).astype(np.int64).reshape(-1)
+
+        def product(r1, r2):
+            return product2(_hdot(A.T, _hchi(r1, len(r1))), _hdot(B, _hchi(r2, len(r2))))
+        return _hlayer(st, C, product, A.shape[0], B.shape[1], s, t, 0, relu)
+
+    def gated(A, B, mode):
+        n, k = A.shape
+        A, B = A.astype(np.int64).reshape(-1), B.astype(np.int64).reshape(-1)
+
+        def product(r1, r2):
+            E = _hchi(r1 + r2, len(r1 + r2))
+            ev, (_, fa, fb) = _hrounds([E, _hfield(A), _hfield(B)], lambda e, a, b: _hmul(e, _hmul(a, b)), 3,
+                                       _draws(st, _lg(n * k)))
+            return ev, _hsum(_hmul(E, _hfield(A * B))), fa, fb
+        return _hlayer(st, A * B, product, n, k, s, t, mode, False)
+
+    if case["op"] == "gate":
+        return [gated(a["A"], a["B"], case["mode"])]
+    if case["op"] == "embed":
+        tok, E = a["tok"], a["E"]
+        n, k, rows = tok.size, _pow2(case["d"]), _pow2(case["vocab"])
+        C = np.zeros((n, k), dtype=np.int64)
+        C[:case["n"], :case["d"]] = E[tok[:case["n"]]].astype(np.int64) * a["scale"]
+
+        def product(r1, r2):
+            weight = [0] * rows
+            for v, x in zip(tok[:case["n"]].tolist(), _hchi(r1, len(r1)).tolist()):
+                weight[v] = (weight[v] + a["scale"] * x) % P
+            e = np.zeros(rows, dtype=U)
+            e[:case["vocab"]] = _hdot(E, _hchi(r2, len(r2))[:case["d"]])
+            return product2(np.array(weight, dtype=U), e)
+        return [_hlayer(st, C.reshape(-1), product, n, k, s, t, case["mode"], False)]
+    gate, up = projection(a["X"], a["Wg"], case["relu"]), projection(a["X"], a["Wu"], False)
+    shape = (a["X"].shape[0], a["Wg"].shape[1])
+    mid = gated(gate["Z"].reshape(shape), up["Z"].reshape(shape), 0)
+    return [gate, up, mid, projection(mid["Z"].reshape(shape), a["Wd"], False)]
