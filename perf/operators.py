@@ -45,7 +45,7 @@ def _gate(name, n, k, s, bits, t, mode=0):
     return dict(name=name, **c) if name else c
 
 
-def _ffn(name, n, d, hidden, t=12, relu=True):
+def _ffn(name, n, d, hidden, t=14, relu=True):
     c = dict(op="ffn", n=n, d=d, hidden=hidden, s=8, t=t, relu=relu)
     return dict(name=name, **c) if name else c
 
@@ -92,7 +92,7 @@ def draw(rng):
     if op == "gate":
         n = _log(rng, 1, 512)
         return _gate("", n, _log(rng, 64, 11008), *rng.choice([(8, 12, 15), (8, 12, -1), (12, 15, 17)]), mode)
-    return _ffn("", _log(rng, 1, 512), _log(rng, 64, 2048), _log(rng, 128, 5461), rng.choice([12, 12, -1]),
+    return _ffn("", _log(rng, 1, 512), _log(rng, 64, 2048), _log(rng, 128, 5461), rng.choice([14, 14, -1]),
                 rng.random() < 0.75)
 
 
