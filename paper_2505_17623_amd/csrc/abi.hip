@@ -188,7 +188,7 @@ ra_status ensure_acc(ra_ctx *c, size_t m)
     c->d_acc = nullptr;
     c->acc_cap = 0;
     if (hipMalloc((void **)&c->d_acc, 2 * m * 8) != hipSuccess) return RA_E_NOMEM;
-    RA_HIP(hipMemset(c->d_acc, 0, 2 * m * 8));
+    launch_fill0(c->d_acc, 2 * m, c->stream);  // on the calls' stream: the null stream would not be ordered with it
     c->acc_cap = 2 * m;
     return RA_OK;
 }
