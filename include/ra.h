@@ -333,6 +333,65 @@ ra_status ra_link_workspace_size(uint64_t z_entries, uint32_t n, uint32_t m, siz
 ra_status ra_link_gather(ra_ctx *ctx, const int32_t *d_Z, uint64_t z_entries, const int32_t *d_src,
                          uint64_t a_entries, int32_t *d_A);
 
+/* ---- Layers with another product than a matrix's ----------------------------
+ * Two products of language models, each as a layer: its call stands in the
+ * place of ra_sumcheck_matmul_prove (optionally after ra_witness_plan), and
+ * the layer's ra_rescale_relu_witness and ra_range_prove follow as always.
+ * Over F_p only, as the gather links; a layer proven with them has no a* that
+ * ra_link_prove could link (RA_E_STATE).  ra_verify_ops verifies them.
+ *
+ * The gated product: C = A B entry by entry, the product of a gated
+ * feed-forward block (A the gate projection's output after its ReLU, B the
+ * other projection's output).  With r = (r1, r2) and N = n k a degree-3
+ * sum-check (Sec. II-D) over the entries x proves
+ *   C~(r1, r2) = sum_x eq(r, x) A(x) B(x)
+ * and ends in A~(rho) and B~(rho).  Challenges: r1 (log n), r2 (log k), rho
+ * (log N), in place of the matrix call's. */
+typedef struct {
+    uint32_t rounds; /* out: log N */
+    uint64_t *evals; /* in: host buffer of 4 log N words; out: g_j(0), .., g_j(3) per round */
+    uint64_t c0;     /* out: claimed sum, C~(r1, r2) */
+    uint64_t a_at;   /* out: A~(rho) */
+    uint64_t b_at;   /* out: B~(rho) */
+} ra_gate_proof;
+
+/*   d_A, d_B  n x k factors, RA_I16 or RA_I32 each, entry (i, j) at i ld + j:
+ *             rows lda / ldb entries apart (at least k, or 0: one row of k
+ *             entries for all n, as a learned scale).  The two may overlap.
+ *   d_C       out, n x k int64 (row-major, contiguous), the exact product.
+ * n, k powers of two (RA_E_INVAL; zero-pad), n k <= 2^31
+ * (RA_E_NOT_IMPLEMENTED).  Workspace: ra_gate_workspace_size (every call of
+ * the layer, for any P), or NULL for the context's own. */
+ra_status ra_gate_prove(ra_ctx *ctx, const void *d_A, ra_dtype a_dtype, uint64_t lda, const void *d_B,
+                        ra_dtype b_dtype, uint64_t ldb, uint32_t n, uint32_t k, int64_t *d_C, void *d_ws,
+                        size_t ws_bytes, ra_gate_proof *out);
+ra_status ra_gate_workspace_size(uint32_t n, uint32_t k, size_t *bytes);
+
+/* The token embedding with scaling: row i of C is scale times row tokens[i] of
+ * the table E (a row of zeros for token -1, which pads n to a power of two),
+ * i.e. the matrix product of the n x vocab matrix S with scale at
+ * (i, tokens[i]), never formed, and E.  Its sum-check is the matrix call's
+ * over V = vocab rounded up to a power of two (E's rows past vocab zero):
+ *   C~(r1, r2) = sum_v W(v) e(v),  W(v) = scale sum_{i: tokens[i] = v} eq(r1, i),
+ *   e(v) = sum_j E[v, j] eq(r2, j).
+ * out as for the matrix call: log_m = log V, a_star = W~(rho) (public data:
+ * the verifier computes it from the tokens), b_star = E~(rho, r2).  Challenges:
+ * r1 (log n), r2 (log k), rho (log V).
+ *   d_tokens  n int32 in [-1, vocab); any other value is not followed (a row
+ *             of zeros) and makes the call's status RA_E_INVAL (a synchronous
+ *             call then consumes nothing).
+ *   d_E       vocab x d int16, rows lde >= d entries apart.
+ *   scale     fixed-point factor, any int32.
+ *   d_C       out, n x k int64, k = d rounded up to a power of two (columns
+ *             past d zero).
+ * n a power of two, vocab, d >= 1 (RA_E_INVAL); vocab <= 2^22, d <= 2^20, n k
+ * <= 2^31 (RA_E_NOT_IMPLEMENTED).  Workspace: ra_embed_workspace_size (every
+ * call of the layer, for any P), or NULL for the context's own. */
+ra_status ra_embed_prove(ra_ctx *ctx, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde,
+                         uint32_t vocab, uint32_t d, int32_t scale, int64_t *d_C, void *d_ws, size_t ws_bytes,
+                         ra_matmul_proof *out);
+ra_status ra_embed_workspace_size(uint32_t n, uint32_t vocab, uint32_t d, size_t *bytes);
+
 /* ---- Commitments to the tables: Pedersen vectors on secp256k1 --------------
  * Sec. II-C commits a vector a by g^a with public generators g of a group in
  * which discrete logarithms are hard; Sec. IV instantiates the group with
@@ -475,6 +534,34 @@ ra_status ra_verify(uint64_t p, uint64_t seed, uint32_t n_layers, const ra_layer
 ra_status ra_verify_stream(uint64_t p, const uint64_t *h_challenges, uint64_t n_challenges, uint32_t n_layers,
                            const ra_layer_public *pub, const ra_layer_tables *tables,
                            const ra_layer_transcript *tr, int32_t *verdict, uint32_t *failed_layer);
+
+/* What a layer's product is, beside its ra_layer_public, for ra_verify_ops.
+ * A zeroed struct with from_a = from_b = -1 is a matrix layer as ra_verify has it. */
+typedef enum { RA_LAYER_MATRIX = 0, RA_LAYER_GATE = 1, RA_LAYER_EMBED = 2 } ra_layer_kind;
+typedef struct {
+    uint32_t kind;         /* ra_layer_kind */
+    int32_t from_a;        /* matrix, gate: the earlier layer whose Z the input A (RA_I32) must equal, -1: none */
+    int32_t from_b;        /* gate: the same for the factor B */
+    ra_dtype b_dtype;      /* gate: RA_I16 or RA_I32 */
+    const void *B;         /* gate: n x k, contiguous, the factor B (A: ra_layer_public) */
+    const ra_gate_proof *gate; /* gate: the product's transcript (the layer's mm is not read) */
+    const int32_t *tokens; /* embed: n tokens (the table is ra_layer_public's B, vocab x d, contiguous) */
+    uint32_t vocab, d;     /* embed */
+    int32_t scale;         /* embed */
+} ra_layer_op;
+
+/* The host verifier for networks with such layers: ra_verify with ops (one
+ * per layer; NULL: all matrix layers).  Gate and embed layers take n, k, s,
+ * relu, round_mode, Z and for gate a_dtype, A from ra_layer_public (m and
+ * chained must be 0, link_src NULL).  Verdicts as ra_verify, with 1 to 3 for
+ * the layer's own product (its chain; its final identity; A~(rho) and
+ * B~(rho), or W~(rho) from the tokens and E~(rho, r2)); 12 also for a gate
+ * entry with |A B| > 2^60, whose product mod p is not the integer's; 13 also
+ * for a token outside [-1, vocab); 14 for
+ * from_a / from_b. */
+ra_status ra_verify_ops(uint64_t p, uint64_t seed, uint32_t n_layers, const ra_layer_public *pub,
+                        const ra_layer_op *ops, const ra_layer_tables *tables, const ra_layer_transcript *tr,
+                        int32_t *verdict, uint32_t *failed_layer);
 
 /* The host verifier for layers proven over F_{p^2} (ra_prove_layer_fp2): the
  * checks of ra_verify with the same verdict numbers, every transcript element

@@ -104,6 +104,9 @@ def lib():
                                                         ctypes.POINTER(LayerInfo)]
         L.orc_verify_layer.argtypes = [ctypes.c_int64] * 3 + [i64p] * 3 + [ctypes.c_int] * 3 + \
             [i64p] * 4 + [u64p] * 3 + [ctypes.POINTER(LayerInfo), u64p, ctypes.c_int64, i64p]
+        L.orc_gate_prove.argtypes = [ctypes.c_int64, i64p, i64p, u64p, u64p, u64p, u64p]
+        L.orc_embed_prove.argtypes = [ctypes.c_int64, i64p, ctypes.c_int64, ctypes.c_int64, i64p, ctypes.c_int64] + \
+            [u64p] * 5
         L.orc_link_prove.argtypes = [ctypes.c_int64, i64p, u64p, ctypes.c_int64, i64p, u64p, ctypes.c_int64, i64p,
                                      u64p, u64p, u64p, u64p]
         L.orc_link_verify.argtypes = [ctypes.c_int64, i64p, u64p, ctypes.c_int64, i64p, ctypes.c_uint64, u64p,
@@ -316,6 +319,59 @@ def verify_link(Z, src, z, a_star, link, chal, cursor=0):
                               int(link["z_at"]) & 0xFFFFFFFFFFFFFFFF, int(link["w_at"]) & 0xFFFFFFFFFFFFFFFF,
                               _ptr(chal, u64), len(chal), _ptr(cur, ctypes.c_int64))
     return int(v), int(cur[0])
+
+
+def _layer_of_product(C, s, relu, mode, chal, cursor, rounds, t_in):
+    """The witness, range check and zero-check of a layer whose exact product
+    is C (n x k) and whose product sum-check has `rounds` rounds: the layer [1]
+    C over one row, its challenges without that sum-check's."""
+    n, k = C.shape
+    lN = (n * k).bit_length() - 1
+    chal = _u64(chal)
+    rest = np.concatenate([chal[cursor:cursor + lN], chal[cursor + lN + rounds:]])
+    out = prove_layer(np.ones((1, 1)), C.reshape(1, -1), s, relu, mode, rest, 0, t_in)
+    for key in ("C", "R", "Rm", "Y", "Z"):
+        out[key] = out[key].reshape(n, k)
+    out.update(n=n, k=k, cursor=cursor + out["cursor"] + rounds)
+    return out
+
+
+def prove_gate_layer(A, B, s, relu, mode, chal, cursor=0, t_in=-1):
+    """A layer whose product is A * B entry by entry (orc_gate_prove)."""
+    A, B = _i64(A), _i64(B)
+    n, k = A.shape
+    lN = (n * k).bit_length() - 1
+    c = _u64(list(chal[cursor:cursor + 2 * lN]) + [0])
+    ev, fin = np.zeros(max(4 * lN, 1), dtype=np.uint64), np.zeros(3, dtype=np.uint64)
+    u64, i64 = ctypes.c_uint64, ctypes.c_int64
+    rc = lib().orc_gate_prove(n * k, _ptr(A, i64), _ptr(B, i64), _ptr(c, u64), _ptr(c[lN:], u64), _ptr(ev, u64),
+                              _ptr(fin, u64))
+    if rc != 0:
+        raise OracleError(rc)
+    out = _layer_of_product(A * B, s, relu, mode, chal, cursor, lN, t_in)
+    assert out["c0"] == int(fin[0])
+    out.update(gate_evals=[int(v) for v in ev[:4 * lN]], a_at=int(fin[1]), b_at=int(fin[2]))
+    return out
+
+
+def prove_embed_layer(tokens, E, scale, s, relu, mode, chal, cursor=0, t_in=-1):
+    """A layer whose product is the scaled embedding of tokens (orc_embed_prove)."""
+    tokens, E = _i64(tokens), _i64(E)
+    n, (vocab, d) = tokens.size, E.shape
+    ln, lk, lv = (n - 1).bit_length(), (d - 1).bit_length(), (vocab - 1).bit_length()
+    c = _u64(list(chal[cursor:cursor + ln + lk + lv]) + [0])
+    ev, fin = np.zeros(max(3 * lv, 1), dtype=np.uint64), np.zeros(3, dtype=np.uint64)
+    u64, i64 = ctypes.c_uint64, ctypes.c_int64
+    rc = lib().orc_embed_prove(n, _ptr(tokens, i64), vocab, d, _ptr(E, i64), int(scale), _ptr(c, u64),
+                               _ptr(c[ln:], u64), _ptr(c[ln + lk:], u64), _ptr(ev, u64), _ptr(fin, u64))
+    if rc != 0:
+        raise OracleError(rc)
+    C = np.zeros((n, 1 << lk), dtype=np.int64)
+    C[tokens >= 0, :d] = scale * E[tokens[tokens >= 0]]
+    out = _layer_of_product(C, s, relu, mode, chal, cursor, lv, t_in)
+    assert out["c0"] == int(fin[0])
+    out.update(mm_evals=[int(v) for v in ev[:3 * lv]], a_star=int(fin[1]), b_star=int(fin[2]))
+    return out
 
 
 def prove_network(workload, layers_out=None, links=False):

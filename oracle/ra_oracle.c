@@ -748,3 +748,79 @@ int orc_link_verify(int64_t na, const int64_t *src, const uint64_t *z, int64_t n
     free(ey);
     return !bad && w == w_at ? 0 : 15;
 }
+
+/* Three factors at a point: eq, A, B (the gated product's summand). */
+static uint64_t summand_gate(const uint64_t *v, const void *ctx)
+{
+    (void)ctx;
+    return fmul(v[0], fmul(v[1], v[2]));
+}
+
+/*
+ * The gated product C = A B entry by entry (N = nA entries): the sum-check of
+ * sum_x eq(r, x) A(x) B(x) with round challenges rho (both of log N values).
+ * evals: 4 words a round; out: c0, A~(rho), B~(rho).
+ */
+int orc_gate_prove(int64_t nA, const int64_t *A, const int64_t *B, const uint64_t *r, const uint64_t *rho,
+                   uint64_t *evals, uint64_t *out)
+{
+    int v = ilog2_exact(nA);
+    if (v < 0) return ORC_E_INVAL;
+    uint64_t *T[3], finals[3];
+    for (int q = 0; q < 3; q++) T[q] = malloc(sizeof(uint64_t) * (size_t)nA);
+    int rc = T[0] && T[1] && T[2] ? ORC_OK : ORC_E_NOMEM;
+    if (rc == ORC_OK) {
+        chi_vector(r, v, T[0]);
+        uint64_t c = 0;
+        for (int64_t x = 0; x < nA; x++) {
+            T[1][x] = fint(A[x]);
+            T[2][x] = fint(B[x]);
+            c = fadd(c, fmul(T[0][x], fmul(T[1][x], T[2][x])));
+        }
+        sumcheck_prove(v, 3, 3, T, summand_gate, NULL, rho, evals, finals);
+        out[0] = c;
+        out[1] = finals[1];
+        out[2] = finals[2];
+    }
+    for (int q = 0; q < 3; q++) free(T[q]);
+    return rc;
+}
+
+/*
+ * The scaled embedding of n tokens (-1: a row of zeros) from E (vocab x d):
+ * the sum-check of sum_v W(v) e(v) over the vocabulary rounded up to a power
+ * of two.  evals: 3 words a round; out: c0, W~(rho), E~(rho, r2).
+ */
+int orc_embed_prove(int64_t n, const int64_t *tok, int64_t vocab, int64_t d, const int64_t *E, int64_t scale,
+                    const uint64_t *r1, const uint64_t *r2, const uint64_t *rho, uint64_t *evals, uint64_t *out)
+{
+    int ln = ilog2_exact(n), lk = 0, lv = 0;
+    while (((int64_t)1 << lk) < d) lk++;
+    while (((int64_t)1 << lv) < vocab) lv++;
+    if (ln < 0 || d < 1 || vocab < 1) return ORC_E_INVAL;
+    for (int64_t i = 0; i < n; i++)
+        if (tok[i] < -1 || tok[i] >= vocab) return ORC_E_INVAL;
+    const int64_t rows = (int64_t)1 << lv;
+    uint64_t *W = calloc((size_t)rows, sizeof(uint64_t)), *e = calloc((size_t)rows, sizeof(uint64_t)), finals[2];
+    if (!W || !e) {
+        free(W);
+        free(e);
+        return ORC_E_NOMEM;
+    }
+    for (int64_t i = 0; i < n; i++)
+        if (tok[i] >= 0) W[tok[i]] = fadd(W[tok[i]], fmul(fint(scale), chi_at(r1, ln, (uint64_t)i)));
+    for (int64_t j = 0; j < d; j++) {
+        const uint64_t x = chi_at(r2, lk, (uint64_t)j);
+        for (int64_t v = 0; v < vocab; v++) e[v] = fadd(e[v], fmul(x, fint(E[v * d + j])));
+    }
+    uint64_t c = 0;
+    for (int64_t v = 0; v < rows; v++) c = fadd(c, fmul(W[v], e[v]));
+    uint64_t *T[2] = {W, e};
+    sumcheck_prove(lv, 2, 2, T, summand_matmul, NULL, rho, evals, finals);
+    out[0] = c;
+    out[1] = finals[0];
+    out[2] = finals[1];
+    free(W);
+    free(e);
+    return ORC_OK;
+}

@@ -43,6 +43,7 @@ struct ra_ctx {
     size_t acc_cap = 0;
     uint64_t r12_off = 0;  // the layer's (r1, r2): offset in the challenge stream
     bool link_ok = false;  // a layer over F_p has just been proven: its a* may be linked (ra_link_prove)
+    bool is_matrix = true;  // the layer's product is a matrix product: its a* is a claim on its input
     sha::Transcript *d_fs = nullptr;  // the Fiat-Shamir transcript (ra_ctx_create_fs), on the device
     size_t eq_cap = 0;
     WitParams *d_params = nullptr;
@@ -196,11 +197,11 @@ ra_status ensure_acc(ra_ctx *c, size_t m)
 // Kernel groups timed with events when profiling is on.
 enum Group {
     G_EQ = 0, G_GEMM, G_BIND_ROWS, G_BIND_COLS, G_MM_ROUNDS, G_MM_TAIL, G_WIT_MINMAX, G_WIT_RESCALE,
-    G_RANGE_SETUP, G_RANGE_PLANE, G_RANGE_ROUNDS, G_RANGE_TAIL, G_FRONT, G_COUNT
+    G_RANGE_SETUP, G_RANGE_PLANE, G_RANGE_ROUNDS, G_RANGE_TAIL, G_FRONT, G_GATE, G_EMBED, G_COUNT
 };
 const char *const kGroupName[G_COUNT] = {
     "eq_table", "gemm_mfma", "bind_rows", "bind_cols", "matmul_rounds", "matmul_tail", "witness_minmax",
-    "witness_rescale", "range_setup", "range_plane", "range_rounds", "range_tail", "matmul_front"};
+    "witness_rescale", "range_setup", "range_plane", "range_rounds", "range_tail", "matmul_front", "gate", "embed"};
 
 hipEvent_t take_event(ra_ctx *c)
 {
@@ -820,6 +821,7 @@ ra_status ra_sumcheck_matmul_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype,
     c->r12_off = c->cursor;
     c->phase = 1;
     c->link_ok = false;
+    c->is_matrix = true;
     c->cursor += need;
     return finish(c, o_tr, [out, lm](const uint64_t *h) {
         out->log_m = (uint32_t)lm;
@@ -1087,7 +1089,7 @@ ra_status ra_range_prove(ra_ctx *c, const uint64_t *d_bits, const int32_t *d_R, 
         launch_xblock(relu != 0, j == 0, xb, jobs, s);
     }
     c->phase = 0;
-    c->link_ok = true;
+    c->link_ok = c->is_matrix;
     c->cursor += need;
     return finish(c, o_tr, [out, R, relu, lN, F_R, RS, Z0, FZ](const uint64_t *h) {
         out->rounds = (uint32_t)R;
@@ -1656,6 +1658,213 @@ extern "C" ra_status ra_link_prove(ra_ctx *c, const int32_t *d_Z, uint64_t z_ent
     if (r != RA_OK && !c->deferred) {  // a refused map consumes nothing
         c->cursor -= (uint64_t)vz;
         c->link_ok = true;
+    }
+    return r;
+}
+
+// ---------------------------------------------------------------------------
+// Layers with another product (gate.hip, embed.hip): their calls stand in the
+// matrix call's place, and the witness and range calls follow as for a matrix.
+// ---------------------------------------------------------------------------
+namespace {
+struct GateLayout {
+    int L, nhs;
+    size_t o_hs, o_ls, o_k, o_t0, o_t1, o_part, bytes;
+};
+GateLayout gate_layout(uint64_t N)
+{
+    GateLayout l;
+    const int lN = log2u(N);
+    l.L = std::min(lN, kXSplitLog);
+    l.nhs = lN > l.L ? 1 << (lN - l.L) : 1;
+    Carve cv;
+    l.o_hs = cv.take<uint64_t>(l.nhs);
+    l.o_ls = cv.take<uint64_t>(2ull << l.L);
+    l.o_k = cv.take<uint64_t>(lN + 1);
+    l.o_t0 = cv.take<uint64_t>(std::max<uint64_t>(N / 2, 1));
+    l.o_t1 = cv.take<uint64_t>(std::max<uint64_t>(N / 2, 1));
+    l.o_part = cv.take<uint64_t>((size_t)std::max(3 * lN, 1) * kGateMaxBlocks);
+    l.bytes = cv.off;
+    return l;
+}
+
+constexpr uint32_t kEmbedMaxVocab = 1u << 22;  // the rounds' partials fit the tail's job list
+constexpr uint32_t kEmbedMaxWidth = 1u << 20;  // exact int64 sums of a row
+struct EmbedLayout {
+    size_t o_b, o_a, o_part, o_bad, bytes;
+};
+EmbedLayout embed_layout(uint64_t rows)
+{
+    EmbedLayout l;
+    Carve cv;
+    l.o_b = cv.take<uint64_t>(rows);
+    l.o_a = cv.take<uint64_t>(rows);
+    l.o_part = cv.take<uint64_t>((size_t)std::max(1, log2u(rows)) * kPartStride);
+    l.o_bad = cv.take<uint64_t>(1);
+    l.bytes = cv.off;
+    return l;
+}
+
+// The layer's state after its product call.
+void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need)
+{
+    c->n = n;
+    c->m = 1;
+    c->k = k;
+    c->r12_off = c->cursor;
+    c->phase = 1;
+    c->link_ok = false;
+    c->is_matrix = false;
+    c->plan.fused = false;
+    c->cursor += need;
+}
+}  // namespace
+
+extern "C" ra_status ra_gate_workspace_size(uint32_t n, uint32_t k, size_t *bytes)
+{
+    if (!bytes || !is_pow2(n) || !is_pow2(k)) return RA_E_INVAL;
+    const uint64_t N = (uint64_t)n * k;
+    if (N > kRangeMaxN) return RA_E_NOT_IMPLEMENTED;
+    *bytes = std::max(gate_layout(N).bytes, range_layout(N, kMaxPlaneLog, 1).bytes);
+    return RA_OK;
+}
+
+extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype, uint64_t lda, const void *d_B,
+                                   ra_dtype b_dtype, uint64_t ldb, uint32_t n, uint32_t k, int64_t *d_C, void *d_ws,
+                                   size_t ws_bytes, ra_gate_proof *out)
+{
+    if (!c || !d_A || !d_B || !d_C || !out) return RA_E_INVAL;
+    if (!is_pow2(n) || !is_pow2(k)) return RA_E_INVAL;
+    if ((a_dtype != RA_I16 && a_dtype != RA_I32) || (b_dtype != RA_I16 && b_dtype != RA_I32)) return RA_E_INVAL;
+    if ((lda && lda < k) || (ldb && ldb < k)) return RA_E_INVAL;
+    const uint64_t N = (uint64_t)n * k;
+    if (N > kRangeMaxN) return RA_E_NOT_IMPLEMENTED;  // the layer's range call could not run
+    if (c->phase != 0) return RA_E_STATE;
+    const int lk = log2u(k), lN = log2u(n) + lk;
+    if (lN && !out->evals) return RA_E_INVAL;
+    const uint64_t need = 2 * (uint64_t)lN;
+    ra_status st = ensure_chal(c, need);
+    if (st != RA_OK) return st;
+    if ((st = ensure_eq(c, (size_t)n + k)) != RA_OK) return st;
+    const GateLayout gl = gate_layout(N);
+    char *ws = nullptr;
+    if ((st = call_ws(c, d_ws, ws_bytes, gl.bytes, &ws)) != RA_OK) return st;
+    size_t o_tr = 0;
+    if ((st = stage_take(c, 3 + 4 * (size_t)lN, &o_tr)) != RA_OK) return st;
+    const uint64_t *r = c->d_chal + c->cursor;
+    GateArgs ga{};
+    ga.A = GateSrc{d_A, lda, a_dtype == RA_I16};
+    ga.B = GateSrc{d_B, ldb, b_dtype == RA_I16};
+    ga.lN = lN;
+    ga.lk = lk;
+    ga.r = r;
+    ga.rho = r + lN;
+    ga.L = gl.L;
+    ga.nhs = gl.nhs;
+    ga.HS = (uint64_t *)(ws + gl.o_hs);
+    ga.LS = (uint64_t *)(ws + gl.o_ls);
+    ga.K = (uint64_t *)(ws + gl.o_k);
+    ga.T0 = (uint64_t *)(ws + gl.o_t0);
+    ga.T1 = (uint64_t *)(ws + gl.o_t1);
+    ga.part = (uint64_t *)(ws + gl.o_part);
+    ga.tr = c->d_stage + o_tr;
+    {
+        Timed tm(c, G_EQ);
+        launch_eq_tables(r, lN - lk, c->d_eq, r + (lN - lk), lk, c->d_eq + n, c->stream);
+    }
+    {
+        Timed tm(c, G_GATE);
+        launch_gate(ga, d_C, c->stream);
+    }
+    begin_layer(c, n, k, need);
+    return finish(c, o_tr, [out, lN](const uint64_t *h) {
+        out->rounds = (uint32_t)lN;
+        out->c0 = h[0];
+        if (lN) std::memcpy(out->evals, h + 1, 4 * (size_t)lN * 8);
+        out->a_at = h[1 + 4 * lN];
+        out->b_at = h[2 + 4 * lN];
+        return (ra_status)RA_OK;
+    });
+}
+
+extern "C" ra_status ra_embed_workspace_size(uint32_t n, uint32_t vocab, uint32_t d, size_t *bytes)
+{
+    if (!bytes || !is_pow2(n) || !vocab || !d) return RA_E_INVAL;
+    if (vocab > kEmbedMaxVocab || d > kEmbedMaxWidth) return RA_E_NOT_IMPLEMENTED;
+    const uint64_t N = (uint64_t)n << log2u(d);
+    if (N > kRangeMaxN) return RA_E_NOT_IMPLEMENTED;
+    *bytes = std::max(embed_layout(1ull << log2u(vocab)).bytes, range_layout(N, kMaxPlaneLog, 1).bytes);
+    return RA_OK;
+}
+
+extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde,
+                                    uint32_t vocab, uint32_t d, int32_t scale, int64_t *d_C, void *d_ws,
+                                    size_t ws_bytes, ra_matmul_proof *out)
+{
+    if (!c || !d_tokens || !d_E || !d_C || !out) return RA_E_INVAL;
+    if (!is_pow2(n) || !vocab || !d || lde < d) return RA_E_INVAL;
+    if (vocab > kEmbedMaxVocab || d > kEmbedMaxWidth) return RA_E_NOT_IMPLEMENTED;
+    const int ln = log2u(n), lk = log2u(d), lv = log2u(vocab);
+    if (((uint64_t)n << lk) > kRangeMaxN) return RA_E_NOT_IMPLEMENTED;  // the layer's range call could not run
+    if (c->phase != 0) return RA_E_STATE;
+    if (lv && !out->evals) return RA_E_INVAL;
+    const uint64_t need = (uint64_t)ln + lk + lv, rows = 1ull << lv;
+    const uint32_t k = 1u << lk;
+    ra_status st = ensure_chal(c, need);
+    if (st != RA_OK) return st;
+    if ((st = ensure_eq(c, (size_t)n + k)) != RA_OK) return st;
+    if ((st = ensure_acc(c, rows)) != RA_OK) return st;
+    const EmbedLayout el = embed_layout(rows);
+    char *ws = nullptr;
+    if ((st = call_ws(c, d_ws, ws_bytes, el.bytes, &ws)) != RA_OK) return st;
+    // transcript: [c0][evals 3 lv][W~][E~][the tokens' status]
+    size_t o_tr = 0;
+    if ((st = stage_take(c, 4 + 3 * (size_t)lv, &o_tr)) != RA_OK) return st;
+    uint64_t *tr = c->d_stage + o_tr;
+    const uint64_t *r1 = c->d_chal + c->cursor, *r2 = r1 + ln, *rho = r2 + lk;
+    EmbedArgs ea{};
+    ea.tok = d_tokens;
+    ea.n = n;
+    ea.E = d_E;
+    ea.ld = lde;
+    ea.vocab = vocab;
+    ea.d = d;
+    ea.lk = lk;
+    ea.scale = scale;
+    ea.rows = rows;
+    ea.E1 = c->d_eq;
+    ea.E2 = c->d_eq + n;
+    ea.acc = c->d_acc;
+    ea.b = (uint64_t *)(ws + el.o_b);
+    ea.bad = (uint32_t *)(ws + el.o_bad);
+    ea.status = tr + 3 + 3 * (size_t)lv;
+    {
+        Timed tm(c, G_EQ);
+        launch_eq_tables(r1, ln, c->d_eq, r2, lk, c->d_eq + n, c->stream, (uint64_t *)(ws + el.o_bad), 1);
+    }
+    {
+        Timed tm(c, G_EMBED);
+        launch_embed_sides(ea, c->stream);
+    }
+    run_instance(c, c->stream, KIND_MATMUL, (uint64_t *)(ws + el.o_a), ea.b, nullptr, lv, rho, tr, 1, 3,
+                 tr + 1 + 3 * lv, 0, (uint64_t *)(ws + el.o_part), G_MM_ROUNDS, G_MM_TAIL, nullptr, nullptr, c->d_acc);
+    {
+        Timed tm(c, G_EMBED);
+        launch_embed_product(ea, d_C, c->stream);
+    }
+    begin_layer(c, n, k, need);
+    const ra_status r = finish(c, o_tr, [out, lv](const uint64_t *h) {
+        if (h[3 + 3 * lv]) return (ra_status)RA_E_INVAL;  // a token outside [-1, vocab)
+        out->log_m = (uint32_t)lv;
+        out->c0 = h[0];
+        if (lv) std::memcpy(out->evals, h + 1, 3 * (size_t)lv * 8);
+        out->a_star = h[1 + 3 * lv];
+        out->b_star = h[2 + 3 * lv];
+        return (ra_status)RA_OK;
+    });
+    if (r != RA_OK && !c->deferred) {  // refused tokens consume nothing
+        c->cursor -= need;
+        c->phase = 0;
     }
     return r;
 }

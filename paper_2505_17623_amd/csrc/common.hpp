@@ -483,6 +483,53 @@ struct LinkArgs {
 void launch_link(const LinkArgs &a, hipStream_t st);
 void launch_link_gather(const int32_t *Z, uint64_t nz, const int32_t *src, uint64_t na, int32_t *A, hipStream_t st);
 
+// ---- the gated product (gate.hip) ----
+constexpr int kGateMaxBlocks = 512;    // blocks of a pass (partials per round)
+constexpr int kGateTailLog = 11;       // the last rounds, over at most 2^11 entries, run from LDS
+constexpr int kGateTailThreads = 512;
+constexpr int kGatePass = 3;           // rounds per pass; the last pass takes what is left
+__host__ __device__ inline int gate_pass_rounds(int left) { return left < kGatePass ? left : kGatePass; }
+__host__ __device__ inline int gate_blocks(uint64_t h)
+{
+    const uint64_t b = (h + kThreads - 1) / kThreads;
+    return (int)(b < (uint64_t)kGateMaxBlocks ? (b ? b : 1) : kGateMaxBlocks);
+}
+struct GateSrc {
+    const void *p;
+    uint64_t ld;               // entries from row to row (0: one row for all)
+    int i16;
+};
+struct GateArgs {
+    GateSrc A, B;              // 2^lN entries, 2^lk columns
+    int lN, lk;
+    const uint64_t *r, *rho;   // (r1, r2) and the rounds' challenges, lN each
+    int L, nhs;                // split of the suffix eq tables (xsetup.hpp)
+    uint64_t *HS, *LS, *K;     // nhs, 2^(L + 1) and lN + 1 words
+    uint64_t *T0, *T1;         // the folded tables: 2^(lN - 1) words each at most
+    uint64_t *part;            // 3 lN x kGateMaxBlocks words
+    uint64_t *tr;              // out: c0, 4 lN round words, A~(rho), B~(rho)
+};
+void launch_gate(const GateArgs &a, int64_t *C, hipStream_t st);
+
+// ---- the token embedding (embed.hip) ----
+struct EmbedArgs {
+    const int32_t *tok;        // n tokens in [-1, vocab)
+    uint32_t n;
+    const int16_t *E;          // vocab x d, rows ld entries apart
+    uint64_t ld;
+    uint32_t vocab, d;
+    int lk;                    // 2^lk columns of C, the first d of them from E
+    int32_t scale;
+    uint64_t rows;             // vocab rounded up to a power of two
+    const uint64_t *E1, *E2;   // eq tables of r1 (n) and r2 (2^lk)
+    uint64_t *acc;             // 2 rows words, zero: W's sums (tail.hpp)
+    uint64_t *b;               // rows words: e(v)
+    uint32_t *bad;             // zero; nonzero if a token is outside
+    uint64_t *status;          // out: that, for the host
+};
+void launch_embed_sides(const EmbedArgs &a, hipStream_t st);
+void launch_embed_product(const EmbedArgs &a, int64_t *C, hipStream_t st);
+
 // ---- launchers (planes.hip) ----
 // The Gram pass works on 16 x 16 tiles of G on and above the diagonal: 3 for
 // up to 32 planes, 6 when P = 64 but only the first 48 planes can hold set

@@ -130,18 +130,95 @@ uint64_t eq_points(const uint64_t *a, const uint64_t *b, int v)
     return acc;
 }
 
+// The integer at x of a matrix of dtype RA_I16 or RA_I32.
+int64_t int_at(const void *p, ra_dtype d, size_t x)
+{
+    return d == RA_I16 ? (int64_t)((const int16_t *)p)[x] : (int64_t)((const int32_t *)p)[x];
+}
+uint64_t mle_matrix(const void *p, ra_dtype d, size_t len, const uint64_t *z, int v)
+{
+    return d == RA_I16 ? mle_ints((const int16_t *)p, len, z, v) : mle_ints((const int32_t *)p, len, z, v);
+}
+
+bool gate_kind(const ra_layer_op *op) { return op && op->kind == RA_LAYER_GATE; }
+bool embed_kind(const ra_layer_op *op) { return op && op->kind == RA_LAYER_EMBED; }
+
+// Rounds of a layer's product (-1: malformed dimensions).
+int product_rounds(const ra_layer_public &L, const ra_layer_op *op)
+{
+    if (!is_pow2(L.n) || !is_pow2(L.k)) return -1;
+    if (gate_kind(op)) return log2u(L.n) + log2u(L.k);
+    if (embed_kind(op)) return op->vocab && op->vocab <= (1u << 31) ? log2u(op->vocab) : -1;
+    return is_pow2(L.m) ? log2u(L.m) : -1;
+}
+
+// Whether A (int32, n x m) is the output Z of the earlier layer `from`.
+bool from_layer(const void *A, ra_dtype d, uint64_t n, uint64_t m, int32_t from, const ra_layer_public *all, uint32_t l)
+{
+    if ((uint32_t)from >= l || !A || d != RA_I32) return false;
+    const ra_layer_public &src = all[from];
+    return src.n == n && src.k == m && std::memcmp(A, src.Z, (size_t)n * m * 4) == 0;
+}
+
+// Checks 1 to 3 of a gated product: its chain, its final identity, the
+// openings of both factors; 12 where an entry's product mod p is not the
+// integer's.
+int verify_gate(const ra_layer_public &L, const ra_layer_op &op, const uint64_t *r, const uint64_t *rho, int lN)
+{
+    const ra_gate_proof &g = *op.gate;
+    const size_t N = (size_t)L.n * L.k;
+    for (size_t x = 0; x < N; x++) {
+        const int64_t c = int_at(L.A, L.a_dtype, x) * int_at(op.B, op.b_dtype, x);
+        if (c > ((int64_t)1 << 60) || c < -((int64_t)1 << 60)) return 12;
+    }
+    uint64_t fin;
+    if (!chain(lN, 3, g.c0, g.evals, rho, &fin)) return 1;
+    if (fin != fmul(eq_points(r, rho, lN), fmul(g.a_at, g.b_at))) return 2;
+    if (mle_matrix(L.A, L.a_dtype, N, rho, lN) != g.a_at || mle_matrix(op.B, op.b_dtype, N, rho, lN) != g.b_at) return 3;
+    return 0;
+}
+
+// Checks 1 to 3 of an embedding: W~(rho) from the tokens, E~(rho, r2) from the table.
+int verify_embed(const ra_layer_public &L, const ra_layer_op &op, const ra_matmul_proof &mm, const uint64_t *r1, int ln,
+                 const uint64_t *r2, int lk, const uint64_t *rho, int lv)
+{
+    uint64_t fin;
+    if (!chain(lv, 2, mm.c0, mm.evals, rho, &fin)) return 1;
+    if (fin != fmul(mm.a_star, mm.b_star)) return 2;
+    const std::vector<uint64_t> e1 = eq_table(r1, ln), e2 = eq_table(r2, lk), ev = eq_table(rho, lv);
+    uint64_t w = 0, b = 0;
+    for (uint32_t i = 0; i < L.n; i++)
+        if (op.tokens[i] >= 0) w = fadd(w, fmul(e1[i], ev[op.tokens[i]]));
+    if (fmul(w, fint(op.scale)) != mm.a_star) return 3;
+    for (uint32_t v = 0; v < op.vocab; v++) {
+        uint64_t row = 0;
+        for (uint32_t j = 0; j < op.d; j++) row = fadd(row, fmul(e2[j], fint(L.B[(size_t)v * op.d + j])));
+        b = fadd(b, fmul(ev[v], row));
+    }
+    return b == mm.b_star ? 0 : 3;
+}
+
+// op (may be null: a matrix layer); all: the network's layers, l this one.
 int verify_layer(const ra_layer_public &L, const ra_layer_tables &T, const ra_layer_transcript &tr,
                  const ra_layer_public *prev, const uint64_t *chal, uint64_t nchal, uint64_t *cursor,
-                 ra_status *err)
+                 ra_status *err, const ra_layer_op *op = nullptr, const ra_layer_public *all = nullptr, uint32_t l = 0)
 {
     const uint32_t n = L.n, m = L.m, k = L.k;
-    if (!is_pow2(n) || !is_pow2(m) || !is_pow2(k) || (!L.A && !L.link_src) || !L.B || !L.Z || !T.R || !T.Rm ||
-        !T.Y || !T.bits)
+    const bool gate = gate_kind(op), embed = embed_kind(op), matrix = !gate && !embed;
+    if (product_rounds(L, op) < 0 || !L.Z || !T.R || !T.Rm || !T.Y || !T.bits) return 13;
+    if (op && (op->kind > RA_LAYER_EMBED || op->from_a < -1 || op->from_b < -1 || (!gate && op->from_b >= 0))) return 13;
+    if (matrix && ((!L.A && !L.link_src) || !L.B)) return 13;
+    if (!matrix && (m || L.chained || L.link_src)) return 13;
+    if (gate && (!L.A || !op->B || !op->gate || (op->b_dtype != RA_I16 && op->b_dtype != RA_I32))) return 13;
+    if (embed) {
+        if (!L.B || !op->tokens || !op->d || op->d > k || (uint64_t)2 * op->d <= k || op->from_a >= 0) return 13;
+        for (uint32_t i = 0; i < n; i++)
+            if (op->tokens[i] < -1 || (op->tokens[i] >= 0 && (uint32_t)op->tokens[i] >= op->vocab)) return 13;
+    }
+    if ((!embed && L.a_dtype != RA_I16 && L.a_dtype != RA_I32) || L.s < 1 || L.s > 30 || L.relu > 1 || L.round_mode > 1)
         return 13;
-    if ((L.a_dtype != RA_I16 && L.a_dtype != RA_I32) || L.s < 1 || L.s > 30 || L.relu > 1 || L.round_mode > 1)
-        return 13;
-    if (L.link_src && L.chained) return 13;
-    const int ln = log2u(n), lm = log2u(m), lk = log2u(k), lN = ln + lk;
+    if (L.link_src && (L.chained || (op && op->from_a >= 0))) return 13;
+    const int ln = log2u(n), lm = product_rounds(L, op), lk = log2u(k), lN = ln + lk;
     const uint64_t N = (uint64_t)n * k;
     const int s = (int)L.s, relu = (int)L.relu, t = tr.wit.t;
     // 14: chaining
@@ -151,6 +228,8 @@ int verify_layer(const ra_layer_public &L, const ra_layer_tables &T, const ra_la
         for (uint64_t i = 0; i < (uint64_t)n * m; i++)
             if (A[i] != prev->Z[i]) return 14;
     }
+    if (op && op->from_a >= 0 && !from_layer(L.A, L.a_dtype, n, matrix ? m : k, op->from_a, all, l)) return 14;
+    if (op && op->from_b >= 0 && !from_layer(op->B, op->b_dtype, n, k, op->from_b, all, l)) return 14;
     // 12: parameters
     if (t < 0 || s + t + 3 > 61 || tr.wit.s != L.s || tr.wit.relu != L.relu || tr.wit.round_mode != L.round_mode)
         return 12;
@@ -161,14 +240,17 @@ int verify_layer(const ra_layer_public &L, const ra_layer_tables &T, const ra_la
         lP++;
     }
     if ((int)tr.wit.P != P || lP > 6) return 12;
-    if (tr.mm.log_m != (uint32_t)lm || tr.rng.rounds != (uint32_t)(lP + lN) ||
+    // the product's transcript, and its words: the sum, the two final values, the rounds
+    const uint32_t p_rounds = gate ? op->gate->rounds : tr.mm.log_m;
+    const uint64_t *p_evals = gate ? op->gate->evals : tr.mm.evals, c0 = gate ? op->gate->c0 : tr.mm.c0;
+    if (p_rounds != (uint32_t)lm || tr.rng.rounds != (uint32_t)(lP + lN) ||
         tr.rng.relu_rounds != (uint32_t)(relu ? lN : 0))
         return 13;
-    if ((lm && !tr.mm.evals) || !tr.rng.evals || (relu && lN && !tr.rng.relu_evals)) return 13;
-    std::vector<uint64_t> words = {tr.mm.c0, tr.mm.a_star, tr.mm.b_star, tr.wit.r_claim, tr.wit.rm_claim,
-                                   tr.wit.y_claim, tr.wit.z_claim, tr.rng.range_sum, tr.rng.bits_claim,
-                                   tr.rng.r_at, tr.rng.y_at};
-    for (int i = 0; i < 3 * lm; i++) words.push_back(tr.mm.evals[i]);
+    if ((lm && !p_evals) || !tr.rng.evals || (relu && lN && !tr.rng.relu_evals)) return 13;
+    std::vector<uint64_t> words = {c0, gate ? op->gate->a_at : tr.mm.a_star, gate ? op->gate->b_at : tr.mm.b_star,
+                                   tr.wit.r_claim, tr.wit.rm_claim, tr.wit.y_claim, tr.wit.z_claim, tr.rng.range_sum,
+                                   tr.rng.bits_claim, tr.rng.r_at, tr.rng.y_at};
+    for (int i = 0; i < (gate ? 4 : 3) * lm; i++) words.push_back(p_evals[i]);
     for (int i = 0; i < 4 * (lP + lN); i++) words.push_back(tr.rng.evals[i]);
     if (relu)
         for (int i = 0; i < 4 * lN; i++) words.push_back(tr.rng.relu_evals[i]);
@@ -186,14 +268,19 @@ int verify_layer(const ra_layer_public &L, const ra_layer_tables &T, const ra_la
     std::vector<uint64_t> r12(r1, r1 + ln);
     r12.insert(r12.end(), r2, r2 + lk);
 
+    // 1-3 of a product other than a matrix's
+    if (!matrix) {
+        const int v = gate ? verify_gate(L, *op, r1, rho, lN) : verify_embed(L, *op, tr.mm, r1, ln, r2, lk, rho, lm);
+        if (v) return v;
+    }
     // 1-2: matrix-multiplication sum-check (Eq. (4))
     uint64_t fin;
-    if (!chain(lm, 2, tr.mm.c0, tr.mm.evals, rho, &fin)) return 1;
-    if (fin != fmul(tr.mm.a_star, tr.mm.b_star)) return 2;
+    if (matrix && !chain(lm, 2, tr.mm.c0, tr.mm.evals, rho, &fin)) return 1;
+    if (matrix && fin != fmul(tr.mm.a_star, tr.mm.b_star)) return 2;
     // 3: a* = A~(r1, rho) (with a gather link: checked by the link, 15), b* = B~(rho, r2)
     std::vector<uint64_t> pa(r1, r1 + ln);
     pa.insert(pa.end(), rho, rho + lm);
-    {
+    if (matrix) {
         std::vector<uint64_t> pb(rho, rho + lm);
         pb.insert(pb.end(), r2, r2 + lk);
         if (!L.link_src) {
@@ -209,7 +296,7 @@ int verify_layer(const ra_layer_public &L, const ra_layer_tables &T, const ra_la
     {
         uint64_t rhs = fadd(fmul(fint((int64_t)1 << s), tr.wit.r_claim), tr.wit.rm_claim);
         if (L.round_mode == RA_ROUND_NEAREST) rhs = fsub(rhs, fint((int64_t)1 << (s - 1)));
-        if (rhs != tr.mm.c0) return 4;
+        if (rhs != c0) return 4;
     }
     // 5-7: concatenated range sum-check
     {
@@ -300,9 +387,9 @@ int verify_layer(const ra_layer_public &L, const ra_layer_tables &T, const ra_la
 
 }  // namespace
 
-extern "C" ra_status ra_verify_stream(uint64_t p, const uint64_t *h_challenges, uint64_t n_challenges,
-                                      uint32_t n_layers, const ra_layer_public *pub, const ra_layer_tables *tables,
-                                      const ra_layer_transcript *tr, int32_t *verdict, uint32_t *failed_layer)
+static ra_status verify_stream(uint64_t p, const uint64_t *h_challenges, uint64_t n_challenges, uint32_t n_layers,
+                               const ra_layer_public *pub, const ra_layer_op *ops, const ra_layer_tables *tables,
+                               const ra_layer_transcript *tr, int32_t *verdict, uint32_t *failed_layer)
 {
     if (!verdict || !failed_layer || (n_layers && (!pub || !tables || !tr)) || (n_challenges && !h_challenges))
         return RA_E_INVAL;
@@ -315,7 +402,7 @@ extern "C" ra_status ra_verify_stream(uint64_t p, const uint64_t *h_challenges, 
     for (uint32_t l = 0; l < n_layers; l++) {
         ra_status err = RA_OK;
         const int v = verify_layer(pub[l], tables[l], tr[l], l ? &pub[l - 1] : nullptr, h_challenges, n_challenges,
-                                   &cursor, &err);
+                                   &cursor, &err, ops ? &ops[l] : nullptr, pub, l);
         if (err != RA_OK) return err;
         if (v) {
             *verdict = v;
@@ -326,6 +413,13 @@ extern "C" ra_status ra_verify_stream(uint64_t p, const uint64_t *h_challenges, 
     return RA_OK;
 }
 
+extern "C" ra_status ra_verify_stream(uint64_t p, const uint64_t *h_challenges, uint64_t n_challenges,
+                                      uint32_t n_layers, const ra_layer_public *pub, const ra_layer_tables *tables,
+                                      const ra_layer_transcript *tr, int32_t *verdict, uint32_t *failed_layer)
+{
+    return verify_stream(p, h_challenges, n_challenges, n_layers, pub, nullptr, tables, tr, verdict, failed_layer);
+}
+
 // The seeded form draws as many challenges as the layers consume (their
 // dimensions and plane counts as stated; a malformed layer fails its own
 // checks before it reads any) and verifies against them.
@@ -333,13 +427,21 @@ extern "C" ra_status ra_verify(uint64_t p, uint64_t seed, uint32_t n_layers, con
                                const ra_layer_tables *tables, const ra_layer_transcript *tr, int32_t *verdict,
                                uint32_t *failed_layer)
 {
+    return ra_verify_ops(p, seed, n_layers, pub, nullptr, tables, tr, verdict, failed_layer);
+}
+
+extern "C" ra_status ra_verify_ops(uint64_t p, uint64_t seed, uint32_t n_layers, const ra_layer_public *pub,
+                                   const ra_layer_op *ops, const ra_layer_tables *tables,
+                                   const ra_layer_transcript *tr, int32_t *verdict, uint32_t *failed_layer)
+{
     if (!verdict || !failed_layer || (n_layers && (!pub || !tables || !tr))) return RA_E_INVAL;
     if (p != kP) return RA_E_UNSUPPORTED_PRIME;
     if (seed == 0) return RA_E_SEED;
     uint64_t total = 0;
     auto lg = [](uint64_t x) { return is_pow2(x) && x <= (1ull << 32) ? log2u(x) : 0; };
     for (uint32_t l = 0; l < n_layers; l++) {
-        const int ln = lg(pub[l].n), lm = lg(pub[l].m), lk = lg(pub[l].k), lN = ln + lk;
+        const int ln = lg(pub[l].n), lk = lg(pub[l].k), lN = ln + lk;
+        const int lm = std::max(product_rounds(pub[l], ops ? &ops[l] : nullptr), 0);
         const int lP = is_pow2(tr[l].wit.P) && tr[l].wit.P <= 128 ? log2u(tr[l].wit.P) : 0;
         total += (uint64_t)ln + lk + lm + 4 + 2 * lP + lN + (pub[l].relu ? lN : 0);
         if (pub[l].link_src && l > 0) total += (uint64_t)lg(pub[l - 1].n) + lg(pub[l - 1].k);
@@ -347,7 +449,7 @@ extern "C" ra_status ra_verify(uint64_t p, uint64_t seed, uint32_t n_layers, con
     std::vector<uint64_t> chal(total ? total : 1);
     ra::ChallengeStream cs(seed);
     for (uint64_t i = 0; i < total; i++) chal[i] = cs.next();
-    return ra_verify_stream(p, chal.data(), total, n_layers, pub, tables, tr, verdict, failed_layer);
+    return verify_stream(p, chal.data(), total, n_layers, pub, ops, tables, tr, verdict, failed_layer);
 }
 
 // ---------------------------------------------------------------------------

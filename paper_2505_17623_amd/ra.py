@@ -31,7 +31,8 @@ EXPORTS = ["ra_ctx_create", "ra_ctx_create_stream", "ra_ctx_destroy", "ra_ctx_cu
            "ra_link_gather", "ra_verify_fs",
            "ra_ctx_create_fs", "ra_prove_layer_fs",
            "ra_commit_generators", "ra_commit_workspace_size", "ra_commit", "ra_commit_open",
-           "ra_commit_batch_workspace_size", "ra_commit_batch"]
+           "ra_commit_batch_workspace_size", "ra_commit_batch",
+           "ra_gate_prove", "ra_gate_workspace_size", "ra_embed_prove", "ra_embed_workspace_size", "ra_verify_ops"]
 
 
 class RAError(RuntimeError):
@@ -77,6 +78,20 @@ class LinkProof(ctypes.Structure):
 
 class LayerTranscript(ctypes.Structure):
     _fields_ = [("mm", MatmulProof), ("wit", WitnessInfo), ("rng", RangeProof), ("link", LinkProof)]
+
+
+class GateProof(ctypes.Structure):
+    _fields_ = [("rounds", ctypes.c_uint32), ("evals", u64p), ("c0", u64), ("a_at", u64), ("b_at", u64)]
+
+
+RA_LAYER_MATRIX, RA_LAYER_GATE, RA_LAYER_EMBED = 0, 1, 2
+
+
+class LayerOp(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_uint32), ("from_a", ctypes.c_int32), ("from_b", ctypes.c_int32),
+                ("b_dtype", ctypes.c_int), ("B", ctypes.c_void_p), ("gate", ctypes.POINTER(GateProof)),
+                ("tokens", ctypes.c_void_p), ("vocab", ctypes.c_uint32), ("d", ctypes.c_uint32),
+                ("scale", ctypes.c_int32)]
 
 
 class Fp2(ctypes.Structure):
@@ -162,7 +177,18 @@ def lib():
         L.ra_verify_fp2.argtypes = [u64, u64, ctypes.c_uint32, ctypes.POINTER(LayerPublic),
                                     ctypes.POINTER(LayerTables), ctypes.POINTER(LayerProofFp2),
                                     ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_uint32)]
-        for f in (L.ra_ctx_create, L.ra_ctx_create_stream, L.ra_workspace_size, L.ra_verify_stream,
+        L.ra_gate_prove.argtypes = [vp, vp, ctypes.c_int, u64, vp, ctypes.c_int, u64, ctypes.c_uint32,
+                                    ctypes.c_uint32, vp, vp, ctypes.c_size_t, ctypes.POINTER(GateProof)]
+        L.ra_gate_workspace_size.argtypes = [ctypes.c_uint32] * 2 + [ctypes.POINTER(ctypes.c_size_t)]
+        L.ra_embed_prove.argtypes = [vp, vp, ctypes.c_uint32, vp, u64, ctypes.c_uint32, ctypes.c_uint32,
+                                     ctypes.c_int32, vp, vp, ctypes.c_size_t, ctypes.POINTER(MatmulProof)]
+        L.ra_embed_workspace_size.argtypes = [ctypes.c_uint32] * 3 + [ctypes.POINTER(ctypes.c_size_t)]
+        L.ra_verify_ops.argtypes = [u64, u64, ctypes.c_uint32, ctypes.POINTER(LayerPublic), ctypes.POINTER(LayerOp),
+                                    ctypes.POINTER(LayerTables), ctypes.POINTER(LayerTranscript),
+                                    ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_uint32)]
+        for f in (L.ra_gate_prove, L.ra_gate_workspace_size, L.ra_embed_prove, L.ra_embed_workspace_size,
+                  L.ra_verify_ops,
+                  L.ra_ctx_create, L.ra_ctx_create_stream, L.ra_workspace_size, L.ra_verify_stream,
                   L.ra_prove_layer_fp2, L.ra_workspace_size_fp2, L.ra_verify_fp2, L.ra_link_prove,
                   L.ra_link_workspace_size, L.ra_link_gather, L.ra_verify_fs, L.ra_ctx_create_fs,
                   L.ra_prove_layer_fs, L.ra_commit_generators, L.ra_commit_workspace_size, L.ra_commit,
@@ -449,6 +475,158 @@ def prove_layer(ctx: Context, A: torch.Tensor, B: torch.Tensor, s: int, relu: bo
     return dict(C=C, R=R, Rm=Rm, Y=Y, Z=Z, bits=bits, transcript=tr)
 
 
+# --- layers with another product than a matrix's ------------------------------
+def _finish_layer(ctx: Context, C, product, s, relu, mode, t, wit, ws):
+    """The witness and range calls that end a layer after its product call."""
+    (R, Rm, Y, Z, bits), info = ra_rescale_relu_witness(ctx, C, s, relu, mode, t, wit, ws)
+    rs = ra_range_prove(ctx, bits, R, Y, info, ws)
+    tr = {}
+
+    def fill():
+        tr.update(product)
+        tr.update(rs)
+        tr.update(t=int(info.t), P=int(info.P), r_claim=int(info.r_claim), rm_claim=int(info.rm_claim),
+                  y_claim=int(info.y_claim), z_claim=int(info.z_claim), s=s, relu=int(bool(relu)), mode=mode)
+    ctx.later(fill)
+    return dict(C=C, R=R, Rm=Rm, Y=Y, Z=Z, bits=bits, transcript=tr)
+
+
+def _layer_outputs(ctx: Context, n, k, s, relu, mode, t, bufs, plan, device):
+    """(C, witness outputs) of a layer, kept in bufs where given; the witness
+    is announced where t is given."""
+    if bufs is not None and "C" not in bufs:
+        bufs["C"] = torch.empty((n, k), dtype=torch.int64, device=device)
+        bufs["wit"] = witness_outputs(n, k, device)
+    C, wit = (bufs["C"], bufs["wit"]) if bufs is not None else (
+        torch.empty((n, k), dtype=torch.int64, device=device), witness_outputs(n, k, device))
+    if t >= 0 and plan:
+        ra_witness_plan(ctx, s, relu, mode, t, wit)
+    return C, wit
+
+
+def _rows(T: torch.Tensor):
+    """(pointer, entries from row to row) of a device matrix whose rows are
+    contiguous: any row stride of at least the row, or one row expanded."""
+    assert T.is_cuda and T.dim() == 2 and (T.shape[1] == 1 or T.stride(1) == 1), "rows must be contiguous"
+    ld = T.stride(0) if T.shape[0] > 1 else T.shape[1]
+    return ctypes.c_void_p(T.data_ptr()), ld
+
+
+def ra_gate_prove(ctx: Context, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor | None = None,
+                  ws: torch.Tensor | None = None):
+    """The gated product's call (ra_gate_prove), in the matrix call's place:
+    C = A * B entry by entry.  A, B: int16 or int32 n x k, rows at any stride
+    (a broadcast row: stride 0).  Returns (C, dict(c0, gate_evals, a_at, b_at)),
+    the dict filled at ctx.sync() in deferred mode."""
+    n, k = A.shape
+    assert B.shape == (n, k)
+    if C is None:
+        C = torch.empty((n, k), dtype=torch.int64, device=A.device)
+    assert C.shape == (n, k) and C.dtype == torch.int64 and C.is_contiguous()
+    lN = (n * k).bit_length() - 1
+    ev = np.zeros(max(4 * lN, 1), dtype=np.uint64)
+    pr = GateProof()
+    pr.evals = ev.ctypes.data_as(u64p)
+    (pa, lda), (pb, ldb) = _rows(A), _rows(B)
+    _check(lib().ra_gate_prove(ctx.h, pa, _DT[A.dtype], lda, pb, _DT[B.dtype], ldb, n, k, _dptr(C), *_ws(ws),
+                               ctypes.byref(pr)), "ra_gate_prove")
+    res = {}
+    ctx.later(lambda: res.update(c0=int(pr.c0), gate_evals=ev[:4 * lN].tolist(), a_at=int(pr.a_at),
+                                 b_at=int(pr.b_at)))
+    return C, res
+
+
+def gate_workspace_size(n: int, k: int) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().ra_gate_workspace_size(n, k, ctypes.byref(v)), "ra_gate_workspace_size")
+    return int(v.value)
+
+
+def prove_gate(ctx: Context, A: torch.Tensor, B: torch.Tensor, s: int, relu: bool = False, mode: int = 0, t: int = -1,
+               bufs: dict | None = None, plan: bool = True, ws: torch.Tensor | None = None):
+    """One layer whose product is A * B entry by entry, rounded by s bits (the
+    gated product of a feed-forward block: A the gate's activation, B the
+    other projection's output).  Arguments, buffers and results as
+    prove_layer; the transcript has gate_evals, a_at, b_at in place of the
+    matrix's."""
+    n, k = A.shape
+    C, wit = _layer_outputs(ctx, n, k, s, relu, mode, t, bufs, plan, A.device)
+    C, pr = ra_gate_prove(ctx, A, B, C, ws)
+    return _finish_layer(ctx, C, pr, s, relu, mode, t, wit, ws)
+
+
+def ra_embed_prove(ctx: Context, tokens: torch.Tensor, E: torch.Tensor, scale: int, C: torch.Tensor | None = None,
+                   ws: torch.Tensor | None = None):
+    """The token embedding's call (ra_embed_prove), in the matrix call's place:
+    row i of C is scale * E[tokens[i]] (zeros for token -1), its width d padded
+    with zeros to a power of two.  tokens: a power of two of int32; E: vocab x d
+    int16, rows at any stride.  Returns (C, dict(c0, mm_evals, a_star, b_star)),
+    the dict filled at ctx.sync() in deferred mode."""
+    assert tokens.dtype == torch.int32 and E.dtype == torch.int16
+    n, (vocab, d) = tokens.numel(), E.shape
+    k = 1 << (d - 1).bit_length()
+    if C is None:
+        C = torch.empty((n, k), dtype=torch.int64, device=E.device)
+    assert C.shape == (n, k) and C.dtype == torch.int64 and C.is_contiguous()
+    lv = (vocab - 1).bit_length()
+    ev = np.zeros(max(3 * lv, 1), dtype=np.uint64)
+    pr = MatmulProof()
+    pr.evals = ev.ctypes.data_as(u64p)
+    pe, lde = _rows(E)
+    _check(lib().ra_embed_prove(ctx.h, _dptr(tokens), n, pe, lde, vocab, d, scale, _dptr(C), *_ws(ws),
+                                ctypes.byref(pr)), "ra_embed_prove")
+    res = {}
+    ctx.later(lambda: res.update(c0=int(pr.c0), mm_evals=ev[:3 * lv].tolist(), a_star=int(pr.a_star),
+                                 b_star=int(pr.b_star)))
+    return C, res
+
+
+def embed_workspace_size(n: int, vocab: int, d: int) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().ra_embed_workspace_size(n, vocab, d, ctypes.byref(v)), "ra_embed_workspace_size")
+    return int(v.value)
+
+
+def prove_embed(ctx: Context, tokens: torch.Tensor, E: torch.Tensor, scale: int, s: int, relu: bool = False,
+                mode: int = 0, t: int = -1, bufs: dict | None = None, plan: bool = True,
+                ws: torch.Tensor | None = None):
+    """One layer whose product is the scaled embedding of tokens, rounded by s
+    bits (scale a factor with s fractional bits: Z = round(scale E[token] /
+    2^s)).  Arguments, buffers and results as prove_layer."""
+    k = 1 << (E.shape[1] - 1).bit_length()
+    C, wit = _layer_outputs(ctx, tokens.numel(), k, s, relu, mode, t, bufs, plan, E.device)
+    C, pr = ra_embed_prove(ctx, tokens, E, scale, C, ws)
+    return _finish_layer(ctx, C, pr, s, relu, mode, t, wit, ws)
+
+
+def prove_gated_ffn(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, s: int,
+                    Wd: torch.Tensor | None = None, gate_relu: bool = True, mode: int = 0, ts=None, bufs=None,
+                    plan: bool = True, ws: torch.Tensor | None = None):
+    """A gated feed-forward block, layer by layer: the gate's projection X Wg
+    (with ReLU unless gate_relu is False), the other projection X Wu, their
+    gated product, and with Wd the projection back.  X: int16 or int32, weights
+    int16, dimensions powers of two (zero-padded); every layer rounds by s bits.
+    ts (optional): the layers' range parameters t; bufs (optional): a list of
+    per-layer output dicts (prove_layer), grown on first use.  Returns the list
+    of layer results, each with its inputs (A, and for the product B)."""
+    count = 3 if Wd is None else 4
+    if bufs is not None:
+        while len(bufs) < count:
+            bufs.append({})
+    t = [-1] * count if ts is None else [int(x) for x in ts]
+    b = [None] * count if bufs is None else bufs
+    gate = prove_layer(ctx, X, Wg, s, gate_relu, mode, t[0], b[0], plan, ws)
+    up = prove_layer(ctx, X, Wu, s, False, mode, t[1], b[1], plan, ws)
+    mid = prove_gate(ctx, gate["Z"], up["Z"], s, False, mode, t[2], b[2], plan, ws)
+    gate["A"] = up["A"] = X
+    mid["A"], mid["B"] = gate["Z"], up["Z"]
+    if Wd is None:
+        return [gate, up, mid]
+    down = prove_layer(ctx, mid["Z"], Wd, s, False, mode, t[3], b[3], plan, ws)
+    down["A"] = mid["Z"]
+    return [gate, up, mid, down]
+
+
 def to_device(a: np.ndarray, device="cuda"):
     return torch.from_numpy(np.ascontiguousarray(a)).to(device)
 
@@ -541,7 +719,13 @@ def ra_verify(challenges, layers):
     """Host verifier.  `challenges` is a seed (int: ra_verify draws the
     stream) or an array of challenges (ra_verify_stream).  `layers` is a
     list of dicts with numpy arrays A, B, Z, R, Rm, Y, bits (uint64 words)
-    and the transcript dict; returns (verdict, failed_layer)."""
+    and the transcript dict; returns (verdict, failed_layer).
+
+    Layers of another product (with a seed only: ra_verify_ops) are told by
+    their dicts: a gated product has "B" an int16 or int32 n x k factor and a
+    transcript with gate_evals; an embedding has "tokens", "scale" and "B" the
+    table.  "from_a" / "from_b" (any layer / a gated product): the index of the
+    earlier layer whose Z that input must equal."""
     seeded = isinstance(challenges, (int, np.integer))
     if not seeded:
         chal, cp = _u64_array(challenges)
@@ -549,13 +733,33 @@ def ra_verify(challenges, layers):
     pubs = (LayerPublic * nl)()
     tabs = (LayerTables * nl)()
     trs = (LayerTranscript * nl)()
+    ops = (LayerOp * nl)()
+    special = False
     keep = []
     for i, L in enumerate(layers):
         tr = L["transcript"]
-        A = np.ascontiguousarray(L["A"])
-        B = np.ascontiguousarray(L["B"], dtype=np.int16)
+        gate, embed = "gate_evals" in tr, L.get("tokens") is not None
+        op = ops[i]
+        op.from_a, op.from_b = L.get("from_a", -1), L.get("from_b", -1)
+        special |= gate or embed or op.from_a >= 0 or op.from_b >= 0
+        B = np.ascontiguousarray(L["B"], dtype=None if gate else np.int16)
+        A = np.zeros((1, 1), dtype=np.int16) if embed else np.ascontiguousarray(L["A"])
         n, m = A.shape
         k = B.shape[1]
+        if gate:
+            gev = np.array(tr["gate_evals"] + [0], dtype=np.uint64)
+            gpr = GateProof(len(tr["gate_evals"]) // 4, gev.ctypes.data_as(u64p), tr["c0"], tr["a_at"], tr["b_at"])
+            op.kind, op.B, op.gate = RA_LAYER_GATE, B.ctypes.data, ctypes.pointer(gpr)
+            op.b_dtype = RA_I16 if B.dtype == np.int16 else RA_I32
+            keep += [gev, gpr]
+            m = 0
+            tr = dict(tr, a_star=0, b_star=0, mm_evals=[])
+        elif embed:
+            tok = np.ascontiguousarray(L["tokens"], dtype=np.int32)
+            op.kind, op.tokens, op.scale = RA_LAYER_EMBED, tok.ctypes.data, int(L["scale"])
+            op.vocab, op.d = B.shape
+            keep.append(tok)
+            n, m, k = tok.size, 0, 1 << (k - 1).bit_length()
         arrs = dict(A=A, B=B, Z=np.ascontiguousarray(L["Z"], dtype=np.int32),
                     R=np.ascontiguousarray(L["R"], dtype=np.int32),
                     Rm=np.ascontiguousarray(np.asarray(L["Rm"]).view(np.uint16)),
@@ -576,7 +780,7 @@ def ra_verify(challenges, layers):
         tabs[i] = LayerTables(arrs["R"].ctypes.data, arrs["Rm"].ctypes.data, arrs["Y"].ctypes.data,
                               arrs["bits"].ctypes.data)
         t = trs[i]
-        t.mm.log_m = m.bit_length() - 1
+        t.mm.log_m = len(tr["mm_evals"]) // 3
         t.mm.c0, t.mm.a_star, t.mm.b_star = tr["c0"], tr["a_star"], tr["b_star"]
         t.mm.evals = mm.ctypes.data_as(u64p)
         t.wit = WitnessInfo(tr["s"], tr["relu"], tr["mode"], tr["t"], tr["P"], tr["r_claim"], tr["rm_claim"],
@@ -596,7 +800,11 @@ def ra_verify(challenges, layers):
             t.link.claim, t.link.z_at, t.link.w_at = lk["claim"], lk["z_at"], lk["w_at"]
     verdict = ctypes.c_int32()
     failed = ctypes.c_uint32()
-    if seeded:
+    if special:
+        assert seeded, "layers of another product are verified with a seed"
+        _check(lib().ra_verify_ops(P61, int(challenges), nl, pubs, ops, tabs, trs, ctypes.byref(verdict),
+                                   ctypes.byref(failed)), "ra_verify_ops")
+    elif seeded:
         _check(lib().ra_verify(P61, int(challenges), nl, pubs, tabs, trs, ctypes.byref(verdict),
                                ctypes.byref(failed)), "ra_verify")
     else:

@@ -1,0 +1,344 @@
+"""The gated product and the scaled token embedding as layers (ra_gate_prove,
+ra_embed_prove) through the C ABI: every transcript word and table bit-exact
+against the oracle over sizes around the kernels' edges, types, strides and
+tokens; both together in a language model's chain of layers, verified; the
+refusals.  All outputs are integers, so every comparison is exact."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from helpers import pack_planes
+from oracle import oracle as orc
+from paper_2505_17623_amd import inputs
+
+pytestmark = pytest.mark.gpu
+P61 = (1 << 61) - 1
+REST = ["t", "P", "c0", "r_claim", "rm_claim", "y_claim", "z_claim", "range_sum", "rs_evals", "bits_claim", "zc_evals",
+        "r_at", "y_at"]
+GATE, EMBED = ["gate_evals", "a_at", "b_at"] + REST, ["mm_evals", "a_star", "b_star"] + REST
+
+
+@pytest.fixture(scope="module")
+def ra():
+    from paper_2505_17623_amd import ra as ra_mod
+    ra_mod.lib()
+    assert torch.cuda.is_available()
+    return ra_mod
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def same(got, want, keys):
+    bad = [k for k in keys if got["transcript"][k] != want[k]]
+    assert not bad, bad
+    for k in ("C", "R", "Y", "Z"):
+        assert np.array_equal(got[k].cpu().numpy().astype(np.int64), want[k]), k
+    assert np.array_equal(got["Rm"].cpu().numpy().view(np.uint16).astype(np.int64), want["Rm"])
+    assert np.array_equal(got["bits"].cpu().numpy().view(np.uint64), pack_planes(want["bits"]))
+
+
+def ints(rng, shape, dtype, top):
+    x = rng.integers(-top, top, shape)
+    x.reshape(-1)[:1] = -top
+    return x.astype(dtype)
+
+
+# --- the gated product ---------------------------------------------------------
+SHAPES = [(1, 1), (1, 2), (2, 1), (4, 4), (1, 512), (64, 16), (1, 2048), (2048, 1), (4, 1024), (64, 128), (256, 64),
+          (8, 4096), (256, 256), (512, 256)]
+
+
+@pytest.mark.parametrize("n,k", SHAPES)
+@pytest.mark.parametrize("relu,mode", [(False, 0), (True, 1)])
+def test_gate_matches_oracle(ra, n, k, relu, mode):
+    rng = np.random.default_rng(n + 7 * k)
+    A, B = ints(rng, (n, k), np.int32, 1 << 14), ints(rng, (n, k), np.int32, 1 << 13)
+    chal = inputs.xorshift64_stream(100 + n + k, 1000)
+    want = orc.prove_gate_layer(A, B, 9, relu, mode, chal, 0)
+    ctx = ra.Context(chal)
+    got = ra.prove_gate(ctx, dev(A), dev(B), 9, relu, mode)
+    same(got, want, GATE)
+    assert ctx.cursor() == want["cursor"]
+
+
+@pytest.mark.parametrize("da,db", [(np.int16, np.int16), (np.int16, np.int32), (np.int32, np.int16)])
+@pytest.mark.parametrize("n,k", [(2, 8), (32, 256)])
+def test_gate_types(ra, da, db, n, k):
+    rng = np.random.default_rng(k)
+    A, B = (ints(rng, (n, k), d, 1 << 15) for d in (da, db))
+    chal = inputs.xorshift64_stream(41, 1000)
+    same(ra.prove_gate(ra.Context(chal), dev(A), dev(B), 12), orc.prove_gate_layer(A, B, 12, False, 0, chal, 0), GATE)
+
+
+def test_gate_extreme_values(ra):
+    """The ends of int32 against small factors (the largest product is 7 2^30,
+    R = 7 2^26 with s = 4: between 2^28 and 2^29, so t = 28), and rows of zeros."""
+    A = np.array([[-2 ** 31, 2 ** 31 - 1, 0, 1], [2 ** 31 - 1, -2 ** 31, 5, 0], [0, 0, 0, 0], [7, -7, 2, -2]] * 512)
+    B = np.array([[1, 1, 9, -2 ** 31], [-1, 1, 0, 3], [0, 0, 0, 0], [2 ** 30, 2 ** 30, -2 ** 31, 0]] * 512)
+    A, B = A.astype(np.int32), B.astype(np.int32)
+    chal = inputs.xorshift64_stream(43, 1000)
+    want = orc.prove_gate_layer(A, B, 4, False, 0, chal, 0)
+    assert want["t"] == 28
+    same(ra.prove_gate(ra.Context(chal), dev(A), dev(B), 4), want, GATE)
+    with pytest.raises(ra.RAError) as e:  # R past int32
+        ra.prove_gate(ra.Context(chal), dev(A), dev(A), 4)
+    assert e.value.code in (-3, -9)
+
+
+@pytest.mark.parametrize("n,k,ld,off", [(4, 8, 8, 1), (16, 128, 200, 3), (64, 64, 129, 0), (128, 64, 64, 2)])
+def test_gate_strides_and_offsets(ra, n, k, ld, off):
+    """Halves of one wide tensor, rows at odd strides, unaligned bases; C and the outputs' buffers as given."""
+    rng = np.random.default_rng(ld)
+    wide = ints(rng, off + n * ld + k, np.int32, 1 << 12)
+    d = dev(wide)
+    A = torch.as_strided(d, (n, k), (ld, 1), off)
+    B = torch.as_strided(d, (n, k), (ld, 1), off + min(k // 2, ld - 1))
+    chal = inputs.xorshift64_stream(47, 1000)
+    want = orc.prove_gate_layer(A.cpu().numpy(), B.cpu().numpy(), 8, True, 0, chal, 0)
+    before = d.clone()
+    same(ra.prove_gate(ra.Context(chal), A, B, 8, True), want, GATE)
+    assert torch.equal(d, before)
+
+
+@pytest.mark.parametrize("n,k", [(8, 4), (256, 128)])
+def test_gate_broadcast_row(ra, n, k):
+    """A learned scale: one row for all (stride 0), on either side, and on both."""
+    rng = np.random.default_rng(n)
+    A, row = ints(rng, (n, k), np.int32, 1 << 14), ints(rng, (1, k), np.int16, 1 << 12)
+    chal = inputs.xorshift64_stream(53, 1000)
+    r = dev(row).expand(n, k)
+    full = np.broadcast_to(row, (n, k))
+    want = orc.prove_gate_layer(A, full, 10, False, 0, chal, 0)
+    same(ra.prove_gate(ra.Context(chal), dev(A), r, 10), want, GATE)
+    want = orc.prove_gate_layer(full, A, 10, False, 0, chal, 0)
+    same(ra.prove_gate(ra.Context(chal), r, dev(A), 10), want, GATE)
+    want = orc.prove_gate_layer(full, full, 10, False, 0, chal, 0)
+    same(ra.prove_gate(ra.Context(chal), r, r, 10), want, GATE)
+
+
+# --- the embedding -----------------------------------------------------------
+@pytest.mark.parametrize("n,vocab,d", [(1, 1, 1), (2, 1, 3), (1, 2, 1), (4, 3, 5), (1, 1000, 64), (32, 1024, 16),
+                                       (64, 1025, 8), (128, 5003, 30), (1, 4097, 300), (1024, 33, 7), (256, 300, 129),
+                                       (16, 40000, 24)])
+@pytest.mark.parametrize("relu,mode", [(False, 0), (True, 1)])
+def test_embed_matches_oracle(ra, n, vocab, d, relu, mode):
+    rng = np.random.default_rng(vocab + d)
+    tok = rng.integers(-1, vocab, n).astype(np.int32)
+    tok[0] = vocab - 1
+    E = ints(rng, (vocab, d), np.int16, 1 << 15)
+    chal = inputs.xorshift64_stream(200 + n + vocab, 1000)
+    want = orc.prove_embed_layer(tok, E, 1234, 8, relu, mode, chal, 0)
+    ctx = ra.Context(chal)
+    same(ra.prove_embed(ctx, dev(tok), dev(E), 1234, 8, relu, mode), want, EMBED)
+    assert ctx.cursor() == want["cursor"]
+
+
+@pytest.mark.parametrize("which", ["one", "none", "two"])
+def test_embed_repeated_and_absent_tokens(ra, which):
+    """Every position the same token (its weight sums all of eq(r1, .)), padding only, two tokens."""
+    rng = np.random.default_rng(5)
+    n, vocab, d = 2048, 500, 12
+    tok = {"one": np.full(n, 321), "none": np.full(n, -1), "two": np.where(rng.random(n) < 0.3, 0, 499)}[which]
+    tok = tok.astype(np.int32)
+    E = ints(rng, (vocab, d), np.int16, 1 << 15)
+    chal = inputs.xorshift64_stream(61, 1000)
+    want = orc.prove_embed_layer(tok, E, -(2 ** 12), 9, False, 0, chal, 0)
+    same(ra.prove_embed(ra.Context(chal), dev(tok), dev(E), -(2 ** 12), 9), want, EMBED)
+
+
+@pytest.mark.parametrize("scale", [0, 1, -1, 2 ** 31 - 1, -(2 ** 31)])
+def test_embed_scales(ra, scale):
+    rng = np.random.default_rng(9)
+    tok, E = rng.integers(0, 77, 16).astype(np.int32), ints(rng, (77, 16), np.int16, 1 << 11)
+    chal = inputs.xorshift64_stream(67, 1000)
+    want = orc.prove_embed_layer(tok, E, scale, 13, False, 0, chal, 0)
+    same(ra.prove_embed(ra.Context(chal), dev(tok), dev(E), scale, 13), want, EMBED)
+
+
+@pytest.mark.parametrize("vocab,d,ld,off", [(100, 16, 24, 0), (100, 16, 17, 1), (37, 5, 8, 3), (2000, 64, 64, 4)])
+def test_embed_table_strides(ra, vocab, d, ld, off):
+    rng = np.random.default_rng(ld)
+    wide = ints(rng, off + vocab * ld, np.int16, 1 << 14)
+    E = torch.as_strided(dev(wide), (vocab, d), (ld, 1), off)
+    tok = rng.integers(-1, vocab, 64).astype(np.int32)
+    chal = inputs.xorshift64_stream(71, 1000)
+    want = orc.prove_embed_layer(tok, E.cpu().numpy(), 999, 8, False, 0, chal, 0)
+    same(ra.prove_embed(ra.Context(chal), dev(tok), E, 999, 8), want, EMBED)
+
+
+# --- modes of use ------------------------------------------------------------
+def test_planned_deferred_repeated(ra):
+    """t given, buffers kept, outputs deferred, three requests in a row on one
+    stream of challenges; with and without the announced witness; the
+    workspace the caller's."""
+    rng = np.random.default_rng(3)
+    n, k, vocab = 32, 64, 700
+    A, B = ints(rng, (n, k), np.int32, 1 << 12), ints(rng, (n, k), np.int32, 1 << 12)
+    tok, E = rng.integers(0, vocab, n).astype(np.int32), ints(rng, (vocab, k), np.int16, 1 << 11)
+    chal = inputs.xorshift64_stream(79, 4000)
+    want, cur = [], 0
+    for _ in range(3):
+        e = orc.prove_embed_layer(tok, E, 300, 8, False, 0, chal, cur, 16)
+        g = orc.prove_gate_layer(A, B, 8, True, 0, chal, e["cursor"], 17)
+        want.append((e, g))
+        cur = g["cursor"]
+    size = max(ra.gate_workspace_size(n, k), ra.embed_workspace_size(n, vocab, k))
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    for plan in (True, False):
+        for deferred in (True, False):
+            ctx = ra.Context(chal, deferred=deferred)
+            for e, g in want:
+                ge = ra.prove_embed(ctx, dev(tok), dev(E), 300, 8, t=16, plan=plan, ws=ws)
+                gg = ra.prove_gate(ctx, dev(A), dev(B), 8, True, t=17, plan=plan, ws=ws)
+                if deferred:
+                    ctx.sync()
+                same(ge, e, EMBED)
+                same(gg, g, GATE)
+            assert ctx.cursor() == cur
+
+
+def test_two_contexts_on_two_streams(ra):
+    """Two callers at once, each on its own stream with kept buffers: the results of each alone."""
+    rng = np.random.default_rng(13)
+    n, k, vocab = 128, 512, 3000
+    A, B = ints(rng, (n, k), np.int32, 1 << 12), ints(rng, (n, k), np.int32, 1 << 12)
+    tok, E = rng.integers(0, vocab, n).astype(np.int32), ints(rng, (vocab, k), np.int16, 1 << 11)
+    dA, dB, dt, dE = dev(A), dev(B), dev(tok), dev(E)
+    torch.cuda.synchronize()
+
+    def calls(seed, stream):
+        with torch.cuda.stream(stream):
+            ctx = ra.Context(seed=seed, stream=stream, deferred=True)
+            out = []
+            for _ in range(3):
+                out.append(ra.prove_gate(ctx, dA, dB, 8, t=17))
+                out.append(ra.prove_embed(ctx, dt, dE, 300, 8, t=16))
+        return ctx, out
+    alone = []
+    for seed in (5, 6):
+        ctx, out = calls(seed, torch.cuda.Stream())
+        ctx.sync()
+        alone.append([(o["transcript"], o["Z"].clone()) for o in out])
+    torch.cuda.synchronize()
+    both = [calls(seed, torch.cuda.Stream()) for seed in (5, 6)]
+    for (ctx, out), a in zip(both, alone):
+        ctx.sync()
+        for o, (tr, Z) in zip(out, a):
+            assert o["transcript"] == tr and torch.equal(o["Z"], Z)
+
+
+@pytest.mark.parametrize("n,vocab,d,hidden,ts", [(1, 50, 12, 16, None), (8, 300, 30, 64, None), (64, 1500, 64, 256, (15, 15, 15, 21, 28, 28))])
+def test_language_model_chain(ra, n, vocab, d, hidden, ts):
+    """Tokens -> scaled embedding -> gated block -> logits, against the oracle
+    layer by layer, and accepted by the verifier with every link named; a
+    changed token or table is rejected.  Given t: |Z| <= 500 600 / 256 < 2^11
+    after the embedding, |G|, |U| <= 64 2^11 90 / 256 < 2^16, so the gated
+    product's R < 2^32 / 2^8, within [-2^22, 2^22) for t = 21 as 26370^2 / 256
+    < 2^22."""
+    rng = np.random.default_rng(n + d)
+    k, s, seed = 1 << (d - 1).bit_length(), 8, 1000 + n
+    tok = rng.integers(0, vocab, n).astype(np.int32)
+    if n > 1:
+        tok[-1] = -1
+    E = ints(rng, (vocab, d), np.int16, 500)
+    Wg, Wu = (ints(rng, (k, hidden), np.int16, 90) for _ in range(2))
+    Wd, Wo = ints(rng, (hidden, k), np.int16, 90), ints(rng, (k, 32), np.int16, 90)
+    ctx = ra.Context(seed=seed, deferred=ts is not None)
+    ts, known = (ts or [-1] * 6), ts is not None
+    e = ra.prove_embed(ctx, dev(tok), dev(E), 600, s, t=ts[0])
+    block = ra.prove_gated_ffn(ctx, e["Z"], dev(Wg), dev(Wu), s, Wd=dev(Wd), ts=ts[1:5] if known else None)
+    logits = ra.prove_layer(ctx, block[-1]["Z"], dev(Wo), s, False, t=ts[5])
+    if known:
+        ctx.sync()
+    chal = inputs.xorshift64_stream(seed, 4000)
+    we = orc.prove_embed_layer(tok, E, 600, s, False, 0, chal, 0, ts[0])
+    wg = orc.prove_layer(we["Z"], Wg, s, True, 0, chal, we["cursor"], ts[1])
+    wu = orc.prove_layer(we["Z"], Wu, s, False, 0, chal, wg["cursor"], ts[2])
+    wm = orc.prove_gate_layer(wg["Z"], wu["Z"], s, False, 0, chal, wu["cursor"], ts[3])
+    wd = orc.prove_layer(wm["Z"], Wd, s, False, 0, chal, wm["cursor"], ts[4])
+    wo = orc.prove_layer(wd["Z"], Wo, s, False, 0, chal, wd["cursor"], ts[5])
+    for got, want, keys in zip([e, *block, logits], (we, wg, wu, wm, wd, wo), (EMBED, EMBED, EMBED, GATE, EMBED, EMBED)):
+        same(got, want, keys)
+
+    def host(r, **more):
+        return dict({x: r[x].cpu().numpy() for x in ("Z", "R", "Rm", "Y", "bits")}, transcript=r["transcript"], **more)
+    z = [r["Z"].cpu().numpy() for r in [e, *block]]
+    layers = [host(e, tokens=tok, B=E, scale=600), host(block[0], A=z[0], B=Wg, from_a=0),
+              host(block[1], A=z[0], B=Wu, from_a=0), host(block[2], A=z[1], B=z[2], from_a=1, from_b=2),
+              host(block[3], A=z[3], B=Wd, from_a=3), host(logits, A=z[4], B=Wo, from_a=4)]
+    assert ra.ra_verify(seed, layers) == (0, 0)
+    other = tok.copy()
+    other[0] = (other[0] + 1) % vocab
+    assert ra.ra_verify(seed, [dict(layers[0], tokens=other), *layers[1:]]) == (3, 0)
+    table = E.copy()
+    table[tok[0], 0] += 1
+    assert ra.ra_verify(seed, [dict(layers[0], B=table), *layers[1:]]) == (3, 0)
+    assert ra.ra_verify(seed, [*layers[:3], dict(layers[3], from_a=2, from_b=1), *layers[4:]]) == (14, 3)
+
+
+def test_refusals(ra):
+    chal = inputs.xorshift64_stream(83, 400)
+    A = torch.full((4, 8), 9, dtype=torch.int32).cuda()
+    C = torch.empty((4, 8), dtype=torch.int64).cuda()
+    tok = torch.zeros(4, dtype=torch.int32).cuda()
+    E = torch.full((10, 8), 9, dtype=torch.int16).cuda()
+    L, p = ra.lib(), lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    ctx = ra.Context(chal)
+    ev = (ctypes.c_uint64 * 64)()
+    pr, mm = ra.GateProof(evals=ev), ra.MatmulProof(evals=ev)
+
+    def gate(a=p(A), ad=2, lda=8, b=p(A), bd=2, ldb=8, n=4, k=8, c=p(C), ws=None, wb=0, out=pr):
+        return L.ra_gate_prove(ctx.h, a, ad, lda, b, bd, ldb, n, k, c, ws, wb, ctypes.byref(out))
+
+    def embed(t=p(tok), n=4, e=p(E), lde=8, vocab=10, d=8, scale=3, c=p(C), ws=None, wb=0, out=mm):
+        return L.ra_embed_prove(ctx.h, t, n, e, lde, vocab, d, scale, c, ws, wb, ctypes.byref(out))
+    for bad in (dict(a=None), dict(b=None), dict(c=None), dict(ad=3), dict(bd=5), dict(lda=7), dict(ldb=1), dict(n=3),
+                dict(k=0), dict(out=ra.GateProof())):
+        assert gate(**bad) == -1, bad
+    assert gate(n=1 << 16, k=1 << 16, lda=1 << 16, ldb=1 << 16) == -9
+    assert gate(ws=p(C), wb=64) == -8
+    for bad in (dict(t=None), dict(e=None), dict(c=None), dict(n=0), dict(n=6), dict(lde=7), dict(vocab=0), dict(d=0),
+                dict(out=ra.MatmulProof())):
+        assert embed(**bad) == -1, bad
+    assert embed(vocab=(1 << 22) + 1) == -9 and embed(d=(1 << 20) + 1, lde=1 << 21) == -9
+    assert embed(ws=p(C), wb=64) == -8
+    assert ctx.cursor() == 0
+    # a token outside the vocabulary: refused, nothing consumed, and the context goes on
+    for v in (10, -2, 2 ** 31 - 1, -(2 ** 31)):
+        bad = tok.clone()
+        bad[2] = v
+        with pytest.raises(ra.RAError) as e:
+            ra.prove_embed(ctx, bad, E, 3, 4)
+        assert e.value.code == -1 and ctx.cursor() == 0
+    want = orc.prove_embed_layer(tok.cpu().numpy(), E.cpu().numpy(), 3, 4, False, 0, chal, 0)
+    same(ra.prove_embed(ctx, tok, E, 3, 4), want, EMBED)
+    # the order of a layer's calls; no gather link after such a layer
+    with pytest.raises(ra.RAError) as e:
+        ra.link_prove(ctx, A, torch.zeros(4, dtype=torch.int32).cuda())
+    assert e.value.code == -7
+    assert gate() == 0
+    assert gate() == -7 and embed() == -7
+    # a range given too small
+    ctx = ra.Context(chal)
+    with pytest.raises(ra.RAError) as e:
+        ra.prove_gate(ctx, A * 1000, A * 1000, 4, t=2)
+    assert e.value.code == -4
+    # challenges that run out, and a transcript context
+    ctx = ra.Context(chal[:5])
+    assert gate() == -5 and embed() == -5
+    ctx = ra.Context(fs_domain=bytes(32))
+    assert gate() == -5 and embed() == -5
+
+
+def test_deferred_bad_token_is_reported_at_sync(ra):
+    tok = torch.tensor([0, 99], dtype=torch.int32).cuda()
+    E = torch.ones((10, 8), dtype=torch.int16).cuda()
+    ctx = ra.Context(seed=4, deferred=True)
+    ra.prove_embed(ctx, tok, E, 3, 4, t=10)
+    with pytest.raises(ra.RAError) as e:
+        ctx.sync()
+    assert e.value.code == -1

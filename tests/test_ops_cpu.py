@@ -1,0 +1,214 @@
+"""Layers of another product than a matrix's (the gated product, the scaled
+token embedding): the oracle against Eq. (1) and the sum-check's definition in
+pure Python, the library's verifier on the oracle's proofs and on tampered
+ones, and the calls' refusals that need no GPU."""
+import copy
+import ctypes
+
+import numpy as np
+import pytest
+
+from helpers import pack_planes
+from oracle import oracle as orc
+from paper_2505_17623_amd import inputs
+
+P61 = (1 << 61) - 1
+
+
+@pytest.fixture(scope="module")
+def ra():
+    from paper_2505_17623_amd import ra as ra_mod
+    ra_mod.lib()
+    return ra_mod
+
+
+def eq(z, y):
+    """eq(z, y) = prod z_i y_i + (1 - z_i)(1 - y_i) over field points (Eq. (1))."""
+    out = 1
+    for a, b in zip(z, y):
+        out = out * (a * b + (1 - a) * (1 - b)) % P61
+    return out
+
+
+def bits_of(i, v):
+    return [(i >> (v - 1 - j)) & 1 for j in range(v)]
+
+
+def mle(table, z):
+    v = len(z)
+    return sum(int(t) * eq(z, bits_of(i, v)) for i, t in enumerate(table)) % P61
+
+
+def round_values(f, v, deg, rho):
+    """g_j(X) = sum over the remaining variables of f(rho_<j, X, y), from the definition."""
+    out = []
+    for j in range(v):
+        for X in range(deg + 1):
+            out.append(sum(f(rho[:j] + [X] + bits_of(y, v - 1 - j)) for y in range(1 << (v - 1 - j))) % P61)
+    return out
+
+
+@pytest.mark.parametrize("n,k", [(1, 1), (1, 4), (4, 1), (2, 4)])
+def test_gate_oracle_is_the_definition(n, k):
+    rng = np.random.default_rng(n * 10 + k)
+    A, B = rng.integers(-2 ** 20, 2 ** 20, (2, n, k))
+    chal = inputs.xorshift64_stream(11 + n, 200)
+    o = orc.prove_gate_layer(A, B, 8, False, 0, chal, 3)
+    v = (n * k).bit_length() - 1
+    c = [int(x) for x in chal[3:3 + 2 * v]]
+    r, rho = c[:v], c[v:]
+    a, b = A.reshape(-1), B.reshape(-1)
+    assert np.array_equal(o["C"], A * B)
+    assert o["c0"] == mle(a * b, r)
+    assert o["gate_evals"] == round_values(lambda z: eq(r, z) * mle(a, z) * mle(b, z), v, 3, rho)
+    assert (o["a_at"], o["b_at"]) == (mle(a, rho), mle(b, rho))
+
+
+@pytest.mark.parametrize("n,vocab,d", [(1, 1, 1), (4, 3, 2), (2, 5, 3), (1, 8, 4)])
+def test_embed_oracle_is_the_definition(n, vocab, d):
+    rng = np.random.default_rng(vocab)
+    tok = rng.integers(-1, vocab, n)
+    E = rng.integers(-2 ** 15, 2 ** 15, (vocab, d))
+    scale = -37
+    chal = inputs.xorshift64_stream(5 + n, 200)
+    o = orc.prove_embed_layer(tok, E, scale, 6, False, 1, chal, 2)
+    ln, lk, lv = (n - 1).bit_length(), (d - 1).bit_length(), (vocab - 1).bit_length()
+    c = [int(x) for x in chal[2:2 + ln + lk + lv]]
+    r1, r2, rho = c[:ln], c[ln:ln + lk], c[ln + lk:]
+    C = np.zeros((n, 1 << lk), dtype=np.int64)
+    for i, t in enumerate(tok):
+        if t >= 0:
+            C[i, :d] = scale * E[t]
+    assert np.array_equal(o["C"], C)
+    W, e = [0] * (1 << lv), [0] * (1 << lv)
+    for i, t in enumerate(tok):
+        if t >= 0:
+            W[t] = (W[t] + scale * eq(r1, bits_of(i, ln))) % P61
+    for v in range(vocab):
+        e[v] = sum(int(E[v, j]) * eq(r2, bits_of(j, lk)) for j in range(d)) % P61
+    assert o["c0"] == mle(C.reshape(-1), r1 + r2) == sum(x * y for x, y in zip(W, e)) % P61
+    assert o["mm_evals"] == round_values(lambda z: mle(W, z) * mle(e, z), lv, 2, rho)
+    assert (o["a_star"], o["b_star"]) == (mle(W, rho), mle(e, rho))
+
+
+def abi(res, **more):
+    return dict(Z=res["Z"].astype(np.int32), R=res["R"].astype(np.int32), Rm=res["Rm"].astype(np.uint16),
+                Y=res["Y"].astype(np.int32), bits=pack_planes(res["bits"]), transcript=res, **more)
+
+
+def network(seed=91, n=4, vocab=11, d=6, hidden=8, s=8):
+    """Tokens -> embedding -> gated block -> logits, proven by the oracle; the
+    layers as ra_verify takes them."""
+    rng = np.random.default_rng(seed)
+    chal = inputs.xorshift64_stream(seed, 4000)
+    k = 1 << (d - 1).bit_length()
+    tok = rng.integers(0, vocab, n)
+    tok[n - 1] = -1
+    E = rng.integers(-600, 600, (vocab, d)).astype(np.int16)
+    Wg, Wu = rng.integers(-300, 300, (2, k, hidden)).astype(np.int16)
+    Wd, Wo = rng.integers(-300, 300, (hidden, k)).astype(np.int16), rng.integers(-300, 300, (k, 16)).astype(np.int16)
+    e = orc.prove_embed_layer(tok, E, 700, s, False, 0, chal, 0)
+    g = orc.prove_layer(e["Z"], Wg, s, True, 0, chal, e["cursor"])
+    u = orc.prove_layer(e["Z"], Wu, s, False, 0, chal, g["cursor"])
+    m = orc.prove_gate_layer(g["Z"], u["Z"], s, False, 0, chal, u["cursor"])
+    w = orc.prove_layer(m["Z"], Wd, s, False, 0, chal, m["cursor"])
+    o = orc.prove_layer(w["Z"], Wo, s, False, 0, chal, w["cursor"])
+    i32 = lambda r: r["Z"].astype(np.int32)  # noqa: E731
+    return seed, [abi(e, tokens=tok, B=E, scale=700), abi(g, A=i32(e), B=Wg, from_a=0), abi(u, A=i32(e), B=Wu, from_a=0),
+                  abi(m, A=i32(g), B=i32(u), from_a=1, from_b=2), abi(w, A=i32(m), B=Wd, from_a=3),
+                  abi(o, A=i32(w), B=Wo, from_a=4)]
+
+
+def test_verifier_accepts_the_network(ra):
+    seed, layers = network()
+    assert ra.ra_verify(seed, layers) == (0, 0)
+    assert ra.ra_verify(seed + 1, layers)[0] != 0
+
+
+def test_verifier_accepts_single_entries(ra):
+    chal = inputs.xorshift64_stream(3, 400)
+    g = orc.prove_gate_layer([[5]], [[-7]], 1, True, 1, chal, 0)
+    e = orc.prove_embed_layer([0], [[9]], 3, 1, False, 0, chal, g["cursor"])
+    layers = [abi(g, A=np.array([[5]], dtype=np.int16), B=np.array([[-7]], dtype=np.int32)),
+              abi(e, tokens=[0], B=np.array([[9]]), scale=3)]
+    assert ra.ra_verify(3, layers) == (0, 0)
+
+
+def change(layers, l, f):
+    out = [dict(L, transcript=copy.copy(L["transcript"])) for L in layers]
+    for key, v in out[l].items():
+        if isinstance(v, np.ndarray):
+            out[l][key] = v.copy()
+    f(out[l])
+    return out
+
+
+def bump(key, i=None):
+    def f(L):
+        tr = L["transcript"]
+        if i is None:
+            tr[key] = (tr[key] + 1) % P61
+        else:
+            tr[key] = [(x + (q == i)) % P61 for q, x in enumerate(tr[key])]
+    return f
+
+
+def test_verifier_rejects_tampering(ra):
+    seed, layers = network()
+
+    def at(key, index, value):
+        def f(L):
+            L[key][index] = value
+        return f
+    E, G = 0, 3
+    cases = [(E, bump("mm_evals", 0), 1), (E, bump("mm_evals", 7), 1), (E, bump("a_star"), 2), (E, bump("c0"), 1),
+             (G, bump("gate_evals", 2), 1), (G, bump("gate_evals", 17), 1), (G, bump("a_at"), 2), (G, bump("c0"), 1),
+             (E, at("B", (int(layers[0]["tokens"][0]), 0), 599), 3),
+             (E, at("tokens", 0, (int(layers[0]["tokens"][0]) + 1) % 11), 3),
+             (E, at("tokens", 1, -1), 3), (E, at("tokens", 0, 11), 13), (E, at("tokens", 0, -2), 13),
+             (E, lambda L: L.update(scale=701), 3), (E, lambda L: L.update(from_a=0), 13),
+             (G, at("A", (0, 1), 12345), 14), (G, at("B", (1, 1), 12345), 14),
+             (G, lambda L: L.update(from_a=3), 14), (G, lambda L: L.update(from_a=2, from_b=1), 14),
+             (G, lambda L: L.update(from_a=-2), 13),
+             (1, lambda L: L.update(from_a=5), 14)]
+    for l, f, want in cases:
+        got = ra.ra_verify(seed, change(layers, l, f))
+        assert got == (want, l), (l, want, got)
+    # both final values changed so that their product holds: the openings catch it
+    tr = layers[G]["transcript"]
+    half = pow(2, P61 - 2, P61)
+    bad = change(layers, G, lambda L: L["transcript"].update(a_at=tr["a_at"] * 2 % P61, b_at=tr["b_at"] * half % P61))
+    assert ra.ra_verify(seed, bad) == (3, G)
+    # a witness table changed behind a gated product
+    assert ra.ra_verify(seed, change(layers, G, at("R", (0, 0), int(layers[G]["R"][0, 0]) + 1)))[1] == G
+
+
+def test_gate_entries_beyond_the_field(ra):
+    """(2^31 - 1)^2 exceeds 2^60: the product mod p no longer is the integer's."""
+    seed, layers = network()
+
+    def f(L):
+        L["A"][0, 0] = L["B"][0, 0] = 2 ** 31 - 1
+        L.update(from_a=-1, from_b=-1)
+    assert ra.ra_verify(seed, change(layers, 3, f)) == (12, 3)
+
+
+def test_workspace_sizes_and_null_arguments(ra):
+    L, size = ra.lib(), ctypes.c_size_t()
+    assert L.ra_gate_workspace_size(4, 8, None) == -1
+    assert L.ra_gate_workspace_size(3, 8, ctypes.byref(size)) == -1
+    assert L.ra_gate_workspace_size(1 << 16, 1 << 16, ctypes.byref(size)) == -9
+    assert L.ra_embed_workspace_size(4, 0, 8, ctypes.byref(size)) == -1
+    assert L.ra_embed_workspace_size(4, 8, 0, ctypes.byref(size)) == -1
+    assert L.ra_embed_workspace_size(6, 8, 8, ctypes.byref(size)) == -1
+    assert L.ra_embed_workspace_size(4, (1 << 22) + 1, 8, ctypes.byref(size)) == -9
+    assert L.ra_embed_workspace_size(4, 8, (1 << 20) + 1, ctypes.byref(size)) == -9
+    assert ra.gate_workspace_size(4, 8) > 0 and ra.embed_workspace_size(1, 7, 5) > 0
+    assert ra.gate_workspace_size(1024, 4096) >= 2 * 8 * 1024 * 4096 // 2
+    pr, mm = ra.GateProof(), ra.MatmulProof()
+    assert L.ra_gate_prove(None, None, 1, 4, None, 1, 4, 4, 4, None, None, 0, ctypes.byref(pr)) == -1
+    assert L.ra_embed_prove(None, None, 4, None, 4, 4, 4, 1, None, None, 0, ctypes.byref(mm)) == -1
+    v, f = ctypes.c_int32(), ctypes.c_uint32()
+    assert L.ra_verify_ops(P61, 1, 1, None, None, None, None, ctypes.byref(v), ctypes.byref(f)) == -1
+    assert L.ra_verify_ops(P61, 0, 0, None, None, None, None, ctypes.byref(v), ctypes.byref(f)) == -5
+    assert L.ra_verify_ops(97, 1, 0, None, None, None, None, ctypes.byref(v), ctypes.byref(f)) == -2
