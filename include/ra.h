@@ -384,7 +384,7 @@ ra_status ra_gate_workspace_size(uint32_t n, uint32_t k, size_t *bytes);
  *   scale     fixed-point factor, any int32.
  *   d_C       out, n x k int64, k = d rounded up to a power of two (columns
  *             past d zero).
- * n a power of two, vocab, d >= 1 (RA_E_INVAL); vocab <= 2^22, d <= 2^20, n k
+ * n a power of two, vocab, d >= 1 (RA_E_INVAL); vocab <= 2^22, d <= 2^17, n k
  * <= 2^31 (RA_E_NOT_IMPLEMENTED).  Workspace: ra_embed_workspace_size (every
  * call of the layer, for any P), or NULL for the context's own. */
 ra_status ra_embed_prove(ra_ctx *ctx, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde,

@@ -1689,17 +1689,18 @@ GateLayout gate_layout(uint64_t N)
 }
 
 constexpr uint32_t kEmbedMaxVocab = 1u << 22;  // the rounds' partials fit the tail's job list
-constexpr uint32_t kEmbedMaxWidth = 1u << 20;  // exact int64 sums of a row
+constexpr uint32_t kEmbedMaxWidth = 1u << 17;  // exact int32 sums of a quarter row's byte products
 struct EmbedLayout {
-    size_t o_b, o_a, o_part, o_bad, bytes;
+    size_t o_b, o_a, o_part, o_limbs, o_bad, bytes;
 };
-EmbedLayout embed_layout(uint64_t rows)
+EmbedLayout embed_layout(uint64_t rows, uint32_t d)
 {
     EmbedLayout l;
     Carve cv;
     l.o_b = cv.take<uint64_t>(rows);
     l.o_a = cv.take<uint64_t>(rows);
     l.o_part = cv.take<uint64_t>((size_t)std::max(1, log2u(rows)) * kPartStride);
+    l.o_limbs = cv.take<uint64_t>(embed_limb_words(d));
     l.o_bad = cv.take<uint64_t>(1);
     l.bytes = cv.off;
     return l;
@@ -1793,7 +1794,7 @@ extern "C" ra_status ra_embed_workspace_size(uint32_t n, uint32_t vocab, uint32_
     if (vocab > kEmbedMaxVocab || d > kEmbedMaxWidth) return RA_E_NOT_IMPLEMENTED;
     const uint64_t N = (uint64_t)n << log2u(d);
     if (N > kRangeMaxN) return RA_E_NOT_IMPLEMENTED;
-    *bytes = std::max(embed_layout(1ull << log2u(vocab)).bytes, range_layout(N, kMaxPlaneLog, 1).bytes);
+    *bytes = std::max(embed_layout(1ull << log2u(vocab), d).bytes, range_layout(N, kMaxPlaneLog, 1).bytes);
     return RA_OK;
 }
 
@@ -1814,7 +1815,7 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
     if (st != RA_OK) return st;
     if ((st = ensure_eq(c, (size_t)n + k)) != RA_OK) return st;
     if ((st = ensure_acc(c, rows)) != RA_OK) return st;
-    const EmbedLayout el = embed_layout(rows);
+    const EmbedLayout el = embed_layout(rows, d);
     char *ws = nullptr;
     if ((st = call_ws(c, d_ws, ws_bytes, el.bytes, &ws)) != RA_OK) return st;
     // transcript: [c0][evals 3 lv][W~][E~][the tokens' status]
@@ -1835,6 +1836,8 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
     ea.E1 = c->d_eq;
     ea.E2 = c->d_eq + n;
     ea.acc = c->d_acc;
+    ea.r2 = r2;
+    ea.limbs = (uint64_t *)(ws + el.o_limbs);
     ea.b = (uint64_t *)(ws + el.o_b);
     ea.bad = (uint32_t *)(ws + el.o_bad);
     ea.status = tr + 3 + 3 * (size_t)lv;

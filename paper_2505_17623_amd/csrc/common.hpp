@@ -523,10 +523,13 @@ struct EmbedArgs {
     uint64_t rows;             // vocab rounded up to a power of two
     const uint64_t *E1, *E2;   // eq tables of r1 (n) and r2 (2^lk)
     uint64_t *acc;             // 2 rows words, zero: W's sums (tail.hpp)
+    const uint64_t *r2;        // lk coordinates
+    uint64_t *limbs;           // embed_limb_words(d) words: the columns' bytes
     uint64_t *b;               // rows words: e(v)
     uint32_t *bad;             // zero; nonzero if a token is outside
     uint64_t *status;          // out: that, for the host
 };
+inline uint32_t embed_limb_words(uint32_t d) { return (d + 31) / 32 * 64; }
 void launch_embed_sides(const EmbedArgs &a, hipStream_t st);
 void launch_embed_product(const EmbedArgs &a, int64_t *C, hipStream_t st);
 
