@@ -355,12 +355,14 @@ int log2_tail() { return log2u(tail_capacity(0)); }
 // sum_out >= 0 the claimed sum to tr[sum_out].  With tail_out given, the
 // tail is not launched: its arguments and jobs go to tail_out / jobs_out for
 // a launch that carries it as extra workgroups.
+// cmax: rounds per launch (0: the kind's own).
 void run_instance(ra_ctx *c, hipStream_t st, int kind, uint64_t *t0, uint64_t *t1, uint64_t *t2, int v,
                   const uint64_t *rho, uint64_t *tr, int ev_base, int width, uint64_t *finals, int sum_out,
                   uint64_t *part, int g_rounds, int g_tail, TailArgs *tail_out = nullptr, XJobs *jobs_out = nullptr,
-                  uint64_t *acc0 = nullptr)
+                  uint64_t *acc0 = nullptr, int cmax = 0)
 {
-    const int cmax = fused_rounds_max(kind), lt = log2_tail();
+    const int lt = log2_tail();
+    if (cmax == 0) cmax = fused_rounds_max(kind);
     XJobs jobs{};
     jobs.part = part;
     jobs.stride = kPartStride;
@@ -1691,7 +1693,7 @@ GateLayout gate_layout(uint64_t N)
 constexpr uint32_t kEmbedMaxVocab = 1u << 22;  // the rounds' partials fit the tail's job list
 constexpr uint32_t kEmbedMaxWidth = 1u << 17;  // exact int32 sums of a quarter row's byte products
 struct EmbedLayout {
-    size_t o_b, o_a, o_part, o_limbs, o_bad, bytes;
+    size_t o_b, o_a, o_part, o_limbs, bytes;
 };
 EmbedLayout embed_layout(uint64_t rows, uint32_t d)
 {
@@ -1701,13 +1703,25 @@ EmbedLayout embed_layout(uint64_t rows, uint32_t d)
     l.o_a = cv.take<uint64_t>(rows);
     l.o_part = cv.take<uint64_t>((size_t)std::max(1, log2u(rows)) * kPartStride);
     l.o_limbs = cv.take<uint64_t>(embed_limb_words(d));
-    l.o_bad = cv.take<uint64_t>(1);
     l.bytes = cv.off;
     return l;
 }
 
-// The layer's state after its product call.
-void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need)
+// The announced witness (ra_witness_plan) of a product computed entry by entry:
+// whether the product's launch takes it.
+bool plan_witness(ra_ctx *c, uint64_t N, uint64_t *E1, uint64_t *E2, WitEpi *we)
+{
+    const auto &pl = c->plan;
+    if (!pl.valid || pl.bits_words < N) return false;
+    *we = WitEpi{(int)pl.s, pl.t, (int)pl.relu, pl.mode == RA_ROUND_NEAREST ? (int64_t)1 << (pl.s - 1) : 0,
+                 E1, E2, pl.R, pl.Rm, pl.Y, pl.Z, pl.bits, (uint64_t *)(c->d_wit + kWitClaims),
+                 (uint32_t *)(c->d_wit + kWitFlags)};
+    return true;
+}
+
+// The layer's state after its product call (fused: its witness is made, with
+// ntiles partials).
+void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need, bool fused, int ntiles)
 {
     c->n = n;
     c->m = 1;
@@ -1716,7 +1730,8 @@ void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need)
     c->phase = 1;
     c->link_ok = false;
     c->is_matrix = false;
-    c->plan.fused = false;
+    c->plan.fused = fused;
+    c->plan.ntiles = (uint32_t)ntiles;
     c->cursor += need;
 }
 }  // namespace
@@ -1769,15 +1784,14 @@ extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype,
     ga.T1 = (uint64_t *)(ws + gl.o_t1);
     ga.part = (uint64_t *)(ws + gl.o_part);
     ga.tr = c->d_stage + o_tr;
-    {
-        Timed tm(c, G_EQ);
-        launch_eq_tables(r, lN - lk, c->d_eq, r + (lN - lk), lk, c->d_eq + n, c->stream);
-    }
+    uint64_t *E1 = c->d_eq, *E2 = c->d_eq + n;
+    WitEpi we{};
+    const bool fused = plan_witness(c, N, E1, E2, &we);
     {
         Timed tm(c, G_GATE);
-        launch_gate(ga, d_C, c->stream);
+        launch_gate(ga, E1, E2, d_C, fused ? &we : nullptr, c->stream);
     }
-    begin_layer(c, n, k, need);
+    begin_layer(c, n, k, need, fused, gate_entries(N, k, d_C, fused ? &we : nullptr));
     return finish(c, o_tr, [out, lN](const uint64_t *h) {
         out->rounds = (uint32_t)lN;
         out->c0 = h[0];
@@ -1822,7 +1836,6 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
     size_t o_tr = 0;
     if ((st = stage_take(c, 4 + 3 * (size_t)lv, &o_tr)) != RA_OK) return st;
     uint64_t *tr = c->d_stage + o_tr;
-    const uint64_t *r1 = c->d_chal + c->cursor, *r2 = r1 + ln, *rho = r2 + lk;
     EmbedArgs ea{};
     ea.tok = d_tokens;
     ea.n = n;
@@ -1830,32 +1843,38 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
     ea.ld = lde;
     ea.vocab = vocab;
     ea.d = d;
+    ea.ln = ln;
     ea.lk = lk;
     ea.scale = scale;
     ea.rows = rows;
+    ea.r = c->d_chal + c->cursor;
     ea.E1 = c->d_eq;
     ea.E2 = c->d_eq + n;
     ea.acc = c->d_acc;
-    ea.r2 = r2;
     ea.limbs = (uint64_t *)(ws + el.o_limbs);
     ea.b = (uint64_t *)(ws + el.o_b);
-    ea.bad = (uint32_t *)(ws + el.o_bad);
     ea.status = tr + 3 + 3 * (size_t)lv;
-    {
-        Timed tm(c, G_EQ);
-        launch_eq_tables(r1, ln, c->d_eq, r2, lk, c->d_eq + n, c->stream, (uint64_t *)(ws + el.o_bad), 1);
-    }
+    c->h_stage[o_tr + 3 + 3 * (size_t)lv] = 0;
     {
         Timed tm(c, G_EMBED);
-        launch_embed_sides(ea, c->stream);
+        launch_embed_front(ea, c->stream);
+        launch_embed_bind(ea, c->stream);
     }
-    run_instance(c, c->stream, KIND_MATMUL, (uint64_t *)(ws + el.o_a), ea.b, nullptr, lv, rho, tr, 1, 3,
-                 tr + 1 + 3 * lv, 0, (uint64_t *)(ws + el.o_part), G_MM_ROUNDS, G_MM_TAIL, nullptr, nullptr, c->d_acc);
+    // the rounds over the vocabulary while its tables exceed the tail, at most
+    // three a launch and evenly (2^17 entries: three rounds 7.1 us, two 4.8, four 14)
+    const int left = std::max(lv - log2_tail(), 0), nl = (left + 2) / 3, per = left ? (left + nl - 1) / nl : 1;
+    TailArgs ta{};
+    XJobs jobs{};
+    run_instance(c, c->stream, KIND_MATMUL, (uint64_t *)(ws + el.o_a), ea.b, nullptr, lv, ea.r + ln + lk, tr, 1, 3,
+                 tr + 1 + 3 * lv, 0, (uint64_t *)(ws + el.o_part), G_MM_ROUNDS, G_MM_TAIL, &ta, &jobs, c->d_acc, per);
+    WitEpi we{};
+    const uint64_t N = (uint64_t)n << lk;
+    const bool fused = plan_witness(c, N, ea.E1, ea.E2, &we);
     {
         Timed tm(c, G_EMBED);
-        launch_embed_product(ea, d_C, c->stream);
+        launch_embed_product(ea, d_C, fused ? &we : nullptr, ta, jobs, c->stream);
     }
-    begin_layer(c, n, k, need);
+    begin_layer(c, n, k, need, fused, embed_entries(N, k, d_C, fused ? &we : nullptr));
     const ra_status r = finish(c, o_tr, [out, lv](const uint64_t *h) {
         if (h[3 + 3 * lv]) return (ra_status)RA_E_INVAL;  // a token outside [-1, vocab)
         out->log_m = (uint32_t)lv;

@@ -509,7 +509,10 @@ struct GateArgs {
     uint64_t *part;            // 3 lN x kGateMaxBlocks words
     uint64_t *tr;              // out: c0, 4 lN round words, A~(rho), B~(rho)
 };
-void launch_gate(const GateArgs &a, int64_t *C, hipStream_t st);
+// The eq tables E1 (r1) and E2 (r2), C and, with we (ra_witness_plan), its
+// witness in gate_entries workgroups' partials, the sum-check.
+int gate_entries(uint64_t N, uint64_t k, const int64_t *C, const WitEpi *we);
+void launch_gate(const GateArgs &a, uint64_t *E1, uint64_t *E2, int64_t *C, const WitEpi *we, hipStream_t st);
 
 // ---- the token embedding (embed.hip) ----
 struct EmbedArgs {
@@ -518,20 +521,24 @@ struct EmbedArgs {
     const int16_t *E;          // vocab x d, rows ld entries apart
     uint64_t ld;
     uint32_t vocab, d;
-    int lk;                    // 2^lk columns of C, the first d of them from E
+    int ln, lk;                // n = 2^ln; 2^lk columns of C, the first d of them from E
     int32_t scale;
     uint64_t rows;             // vocab rounded up to a power of two
-    const uint64_t *E1, *E2;   // eq tables of r1 (n) and r2 (2^lk)
+    const uint64_t *r;         // r1, r2
+    uint64_t *E1, *E2;         // out: eq tables of r1 (n) and r2 (2^lk)
     uint64_t *acc;             // 2 rows words, zero: W's sums (tail.hpp)
-    const uint64_t *r2;        // lk coordinates
-    uint64_t *limbs;           // embed_limb_words(d) words: the columns' bytes
+    uint64_t *limbs;           // embed_limb_words(d) words: eq(r2, .) in bytes
     uint64_t *b;               // rows words: e(v)
-    uint32_t *bad;             // zero; nonzero if a token is outside
-    uint64_t *status;          // out: that, for the host
+    uint64_t *status;          // set if a token is outside (host memory, cleared by the host)
 };
 inline uint32_t embed_limb_words(uint32_t d) { return (d + 31) / 32 * 64; }
-void launch_embed_sides(const EmbedArgs &a, hipStream_t st);
-void launch_embed_product(const EmbedArgs &a, int64_t *C, hipStream_t st);
+void launch_embed_front(const EmbedArgs &a, hipStream_t st);
+void launch_embed_bind(const EmbedArgs &a, hipStream_t st);
+// C and, with we (ra_witness_plan), its witness in embed_entries workgroups'
+// partials; ta, jobs: the tail of the sum-check, run beside them
+int embed_entries(uint64_t N, uint64_t k, const int64_t *C, const WitEpi *we);
+void launch_embed_product(const EmbedArgs &a, int64_t *C, const WitEpi *we, const TailArgs &ta, const XJobs &jobs,
+                          hipStream_t st);
 
 // ---- launchers (planes.hip) ----
 // The Gram pass works on 16 x 16 tiles of G on and above the diagonal: 3 for

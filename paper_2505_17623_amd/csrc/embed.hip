@@ -12,32 +12,14 @@
 #include <algorithm>
 
 #include "common.hpp"
+#include "entries.hpp"
 #include "m61.hpp"
-#include "ra.h"
+#include "tail.hpp"
+#include "xsetup.hpp"
 
 namespace ra {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-
-// W's sums: W(v) mod p is acc[v] + 2^32 acc[rows + v] (tail.hpp), each word a
-// sum of values below 2^32, so no add wraps and their order does not matter.
-// A token outside [-1, vocab) is not followed: it sets *bad.
-__global__ __launch_bounds__(256) void k_embed_scatter(const int32_t *__restrict__ tok, uint32_t n, uint32_t vocab,
-                                                       uint64_t rows, const uint64_t *__restrict__ E1, uint64_t scale,
-                                                       unsigned long long *__restrict__ acc, uint32_t *__restrict__ bad)
-{
-    for (uint32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
-        const int32_t v = tok[i];
-        if (v < -1 || (v >= 0 && (uint32_t)v >= vocab)) {
-            atomicOr(bad, 1u);
-            continue;
-        }
-        if (v < 0) continue;
-        const uint64_t e = m61::mul(E1[i], scale);
-        atomicAdd(acc + v, (unsigned long long)(e & 0xFFFFFFFFull));
-        atomicAdd(acc + rows + v, (unsigned long long)(e >> 32));
-    }
-}
 
 // e(v) = sum_j E[v, j] e_j (e_j = eq(r2, j), zero past d) on the matrix cores.
 // A row of the table is taken as 2 d bytes, as it lies in memory: with E = 256
@@ -57,20 +39,68 @@ __device__ __forceinline__ uint32_t limb_byte(uint64_t e, int c)
     return (uint32_t)(((e + C) ^ C) >> (8 * c)) & 0xFFu;
 }
 
-__global__ __launch_bounds__(256) void k_embed_limbs(const uint64_t *__restrict__ E2, uint32_t d, uint32_t count,
-                                                     v4i *__restrict__ limbs)
+__device__ __forceinline__ void embed_limbs(const uint64_t *r2, int lk, uint32_t d, uint32_t t, v4i *__restrict__ limbs)
 {
-    const uint32_t t = blockIdx.x * blockDim.x + threadIdx.x;  // (4 q + g) 8 + c
-    if (t >= count) return;
-    const uint32_t j0 = t & ~7u;
-    const int c = t & 7;
+    const uint32_t j0 = t & ~7u;  // t = (4 q + g) 8 + c
+    const int c = t & 7, low = lk < 3 ? lk : 3;
+    // eq(r2, j0 + u): the coordinates above the last three once, then those
+    uint64_t e[8];
+    e[0] = j0 < d ? eq_suffix(r2, 0, lk - low, j0 >> low) : 0;
+    for (int i = 0; i < low; i++) {
+        const uint64_t z = r2[lk - low + i];
+#pragma unroll
+        for (int u = 3; u >= 0; u--)
+            if (u < 1 << i) {
+                e[2 * u + 1] = m61::lmul(e[u], z);
+                e[2 * u] = m61::lsub(e[u], e[2 * u + 1]);
+            }
+    }
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int u = 0; u < 8; u++) {
-        const uint64_t e = j0 + u < d ? E2[j0 + u] : 0;
-        w[u >> 1] |= (limb_byte(e, c) | limb_byte(m61::rotl(e, 8), c) << 8) << (16 * (u & 1));
+        const uint64_t x = u < 1 << low && j0 + u < d ? m61::canon(e[u]) : 0;
+        w[u >> 1] |= (limb_byte(x, c) | limb_byte(m61::rotl(x, 8), c) << 8) << (16 * (u & 1));
     }
     limbs[t] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+}
+
+// All that depends on the challenges alone, and W's sums: nl threads write the
+// columns' fragments, the next n and 2^lk the eq tables E1 and E2, the last n
+// (one a token) add eq(r1, i) scale to W(tok[i]).  W(v) mod p is acc[v] + 2^32
+// acc[rows + v] (tail.hpp), each word a sum of values below 2^32, so no add
+// wraps and their order does not matter.  A token outside [-1, vocab) is not
+// followed; it sets *status.
+__global__ __launch_bounds__(256) void k_embed_front(EmbedArgs a, uint32_t nl, uint64_t scale)
+{
+    __shared__ uint64_t rl[64];
+    const int ln = a.ln, lk = a.lk, tid = threadIdx.x;
+    if (tid < ln + lk) rl[tid] = a.r[tid];
+    __syncthreads();
+    uint64_t i = (uint64_t)blockIdx.x * blockDim.x + tid;
+    if (i < nl) {
+        embed_limbs(rl + ln, lk, a.d, (uint32_t)i, (v4i *)a.limbs);
+        return;
+    }
+    i -= nl;
+    if (i < a.n) {
+        a.E1[i] = eq_suffix(rl, 0, ln, i);
+        return;
+    }
+    i -= a.n;
+    if (i < 1ull << lk) {
+        a.E2[i] = eq_suffix(rl, ln, lk, i);
+        return;
+    }
+    i -= 1ull << lk;
+    if (i >= a.n) return;
+    const int32_t v = a.tok[i];
+    if (v < 0 || (uint32_t)v >= a.vocab) {
+        if (v != -1) *a.status = 1;
+        return;
+    }
+    const uint64_t e = m61::mul(eq_suffix(rl, 0, ln, i), scale);
+    atomicAdd((unsigned long long *)a.acc + v, (unsigned long long)(e & 0xFFFFFFFFull));
+    atomicAdd((unsigned long long *)a.acc + a.rows + v, (unsigned long long)(e >> 32));
 }
 
 // sum_{j < d} eq(r2, j) from the coordinates of r2 (lk of them): for every set
@@ -159,43 +189,86 @@ __global__ __launch_bounds__(256) void k_embed_bind(const int16_t *__restrict__ 
     b[v0 + tid] = m61::canon(s);
 }
 
-// C, n x 2^lk, and the tokens' status to *status (after the scatter, so *bad
-// is final).
-__global__ __launch_bounds__(256) void k_embed_product(const int32_t *__restrict__ tok, const int16_t *__restrict__ E,
-                                                       uint64_t ld, uint32_t vocab, uint32_t d, int32_t scale, uint64_t N,
-                                                       int lk, int64_t *__restrict__ C, const uint32_t *__restrict__ bad,
-                                                       uint64_t *__restrict__ status)
-{
-    if (blockIdx.x == 0 && threadIdx.x == 0) *status = *bad;
-    for (uint64_t x = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; x < N; x += (uint64_t)gridDim.x * blockDim.x) {
-        const int32_t v = tok[x >> lk];
-        const uint32_t j = (uint32_t)(x & ((1ull << lk) - 1));
-        C[x] = v >= 0 && (uint32_t)v < vocab && j < d ? (int64_t)scale * E[(uint64_t)v * ld + j] : 0;
+// V entries of C: scale times the token's row, zero past d, for token -1 and
+// for one outside the vocabulary.
+template <int V> struct EmbedRows {
+    const int32_t *tok;
+    const int16_t *E;
+    uint64_t ld;
+    uint32_t vocab, d;
+    int32_t scale;
+    __device__ __forceinline__ void operator()(uint64_t row, uint64_t col, int64_t (&c)[V]) const
+    {
+        const int32_t v = tok[row];
+        int16_t h[V] = {};
+        if (v >= 0 && (uint32_t)v < vocab && col < d) {
+            const int16_t *p = E + (uint64_t)v * ld + col;
+            if (col + V <= d) {
+                __builtin_memcpy(h, p, sizeof h);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i++)
+                    if (col + i < d) h[i] = p[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) c[i] = (int64_t)scale * h[i];
     }
+};
+
+// The product (with the witness), and the sum-check's last rounds as its first
+// workgroups.
+template <int V, bool WIT>
+__global__ __launch_bounds__(256) void k_embed_product(EmbedArgs a, int64_t *C, WitEpi we, TailArgs ta, XJobs jobs,
+                                                       int ntail)
+{
+    __shared__ uint64_t smem[kTailSmem];
+    static_assert(kTailSmem >= entries_lds_words(kThreads), "the tail's LDS serves the product");
+    if ((int)blockIdx.x < ntail) {  // workgroup-uniform
+        tail_block<KIND_MATMUL>(ta, jobs, blockIdx.x, smem);
+        return;
+    }
+    entries_block<V, WIT, kThreads>(EmbedRows<V>{a.tok, a.E, a.ld, a.vocab, a.d, a.scale}, a.n, a.lk, C, we,
+                                    (int)blockIdx.x - ntail, (int)gridDim.x - ntail, smem);
 }
 
-void launch_embed_sides(const EmbedArgs &a, hipStream_t st)
+void launch_embed_front(const EmbedArgs &a, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_embed_scatter, dim3((unsigned)std::min<uint64_t>((a.n + 255) / 256, 1024)), dim3(256), 0, st,
-                       a.tok, a.n, a.vocab, a.rows, a.E1, a.scale < 0 ? m61::P - (uint64_t)(-(int64_t)a.scale) : (uint64_t)a.scale,
-                       (unsigned long long *)a.acc, a.bad);
-    const uint32_t count = embed_limb_words(a.d) / 2;
-    hipLaunchKernelGGL(k_embed_limbs, dim3((count + 255) / 256), dim3(256), 0, st, a.E2, a.d, count, (v4i *)a.limbs);
+    const uint64_t scale = a.scale < 0 ? m61::P - (uint64_t)(-(int64_t)a.scale) : (uint64_t)a.scale;
+    const uint32_t nl = embed_limb_words(a.d) / 2;
+    const uint64_t threads = nl + 2 * (uint64_t)a.n + (1ull << a.lk);
+    hipLaunchKernelGGL(k_embed_front, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a, nl, scale);
+}
+
+void launch_embed_bind(const EmbedArgs &a, hipStream_t st)
+{
+    const uint64_t *r2 = a.r + a.ln;
     // 64 rows a workgroup use each fragment of the columns four times; 16 rows
     // where 64 would leave CUs without a workgroup
     if (a.rows >= 64 * 256)
         hipLaunchKernelGGL((k_embed_bind<4, 4>), dim3((unsigned)(a.rows / 64)), dim3(256), 0, st, a.E, a.ld, a.vocab,
-                           a.d, a.rows, (const v4i *)a.limbs, a.r2, a.lk, a.b);
+                           a.d, a.rows, (const v4i *)a.limbs, r2, a.lk, a.b);
     else
         hipLaunchKernelGGL((k_embed_bind<1, 8>), dim3((unsigned)((a.rows + 15) / 16)), dim3(256), 0, st, a.E, a.ld,
-                           a.vocab, a.d, a.rows, (const v4i *)a.limbs, a.r2, a.lk, a.b);
+                           a.vocab, a.d, a.rows, (const v4i *)a.limbs, r2, a.lk, a.b);
 }
 
-void launch_embed_product(const EmbedArgs &a, int64_t *C, hipStream_t st)
+int embed_entries(uint64_t N, uint64_t k, const int64_t *C, const WitEpi *we)
 {
-    const uint64_t N = (uint64_t)a.n << a.lk;
-    hipLaunchKernelGGL(k_embed_product, dim3((unsigned)std::min<uint64_t>((N + 255) / 256, 4096)), dim3(256), 0, st,
-                       a.tok, a.E, a.ld, a.vocab, a.d, a.scale, N, a.lk, C, a.bad, a.status);
+    return entries_blocks(N, entries_width(k, C, we), kThreads);
+}
+
+void launch_embed_product(const EmbedArgs &a, int64_t *C, const WitEpi *we, const TailArgs &ta, const XJobs &jobs,
+                          hipStream_t st)
+{
+    const uint64_t k = 1ull << a.lk;
+    const int V = entries_width(k, C, we), ntail = 1 + jobs.nslot;
+    const dim3 grid(ntail + embed_entries(a.n * k, k, C, we)), blk(kThreads);
+    const WitEpi w = we ? *we : WitEpi{};
+    if (V == 2 && we) hipLaunchKernelGGL((k_embed_product<2, true>), grid, blk, 0, st, a, C, w, ta, jobs, ntail);
+    else if (V == 2) hipLaunchKernelGGL((k_embed_product<2, false>), grid, blk, 0, st, a, C, w, ta, jobs, ntail);
+    else if (we) hipLaunchKernelGGL((k_embed_product<1, true>), grid, blk, 0, st, a, C, w, ta, jobs, ntail);
+    else hipLaunchKernelGGL((k_embed_product<1, false>), grid, blk, 0, st, a, C, w, ta, jobs, ntail);
 }
 
 }  // namespace ra

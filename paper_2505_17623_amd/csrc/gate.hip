@@ -15,6 +15,7 @@
 
 #include "assemble.hpp"
 #include "common.hpp"
+#include "entries.hpp"
 #include "m61.hpp"
 #include "xpair.hpp"
 #include "xsetup.hpp"
@@ -29,15 +30,33 @@ __device__ __forceinline__ int32_t gate_load(const GateSrc &s, uint64_t x, int l
     return s.i16 ? (int32_t)((const int16_t *)s.p)[at] : ((const int32_t *)s.p)[at];
 }
 
-// C = A B, exact in int64 (|C| <= 2^62).
-__global__ __launch_bounds__(256) void k_gate_product(GateSrc A, GateSrc B, uint64_t N, int lk, int64_t *__restrict__ C)
-{
-    for (uint64_t x = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; x < N; x += (uint64_t)gridDim.x * blockDim.x)
-        C[x] = (int64_t)gate_load(A, x, lk) * gate_load(B, x, lk);
-}
+// V entries of C = A B, exact in int64 (|C| <= 2^62).
+template <int V> struct GateProduct {
+    GateSrc A, B;
+    __device__ __forceinline__ void factor(const GateSrc &s, uint64_t at, int32_t (&v)[V]) const
+    {
+        if (s.i16) {  // uniform; the loads need no more alignment than the entries have
+            int16_t h[V];
+            __builtin_memcpy(h, (const int16_t *)s.p + at, sizeof h);
+#pragma unroll
+            for (int i = 0; i < V; i++) v[i] = h[i];
+        } else {
+            __builtin_memcpy(v, (const int32_t *)s.p + at, sizeof v);
+        }
+    }
+    __device__ __forceinline__ void operator()(uint64_t row, uint64_t col, int64_t (&c)[V]) const
+    {
+        int32_t a[V], b[V];
+        factor(A, row * A.ld + col, a);
+        factor(B, row * B.ld + col, b);
+#pragma unroll
+        for (int i = 0; i < V; i++) c[i] = (int64_t)a[i] * b[i];
+    }
+};
 
-// The suffix eq tables of r and the prefix products K_j (xsetup.hpp).
-__global__ __launch_bounds__(256) void k_gate_setup(XSetupArgs a)
+// The suffix eq tables of r and the prefix products K_j (xsetup.hpp) by the
+// first nx threads, the eq tables E1 (r1) and E2 (r2) by the others.
+__global__ __launch_bounds__(256) void k_gate_setup(XSetupArgs a, int nx, int ln, uint64_t *E1, uint64_t *E2)
 {
     __shared__ uint64_t rl[64], sl[64];
     if ((int)threadIdx.x < a.lN) {
@@ -45,17 +64,23 @@ __global__ __launch_bounds__(256) void k_gate_setup(XSetupArgs a)
         sl[threadIdx.x] = a.sigx[threadIdx.x];
     }
     __syncthreads();
-    x_setup_body(a, blockIdx.x * blockDim.x + threadIdx.x, rl, sl, sl);
+    const uint64_t g = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (g < (uint64_t)nx) {  // nx a multiple of the workgroup
+        x_setup_body(a, (int)g, rl, sl, sl);
+        return;
+    }
+    const uint64_t i = g - nx, n = 1ull << ln;
+    if (i < n) E1[i] = eq_suffix(rl, 0, ln, i);
+    else if (i - n < 1ull << (a.lN - ln)) E2[i - n] = eq_suffix(rl, ln, a.lN - ln, i - n);
 }
 
 // R rounds j .. j + R - 1 over tables of 2^R q entries in one pass: a thread
 // holds the 2^R entries i + t q that end in entry i of the folded tables.  The
 // first pass reads the factors themselves.
 template <int R, bool FIRST>
-__global__ __launch_bounds__(256) void k_gate_pass(GateArgs a, int j, uint64_t q)
+__device__ __forceinline__ void gate_pass_block(const GateArgs &a, int j, uint64_t q, int blk, int nblk, uint64_t *red)
 {
     constexpr int NL = 1 << R;
-    __shared__ uint64_t red[m61::block_sum_words(3 * R, kThreads)];
     uint64_t rho[R], rr[R], acc[3 * R];
 #pragma unroll
     for (int c = 0; c < R; c++) {
@@ -65,7 +90,7 @@ __global__ __launch_bounds__(256) void k_gate_pass(GateArgs a, int j, uint64_t q
 #pragma unroll
     for (int c = 0; c < 3 * R; c++) acc[c] = 0;
     const int nvar = a.lN - j - R;
-    for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < q; i += (uint64_t)gridDim.x * blockDim.x) {
+    for (uint64_t i = (uint64_t)blk * kThreads + threadIdx.x; i < q; i += (uint64_t)nblk * kThreads) {
         uint64_t u[NL], v[NL], w[NL];
 #pragma unroll
         for (int t = 0; t < NL; t++) {
@@ -89,7 +114,28 @@ __global__ __launch_bounds__(256) void k_gate_pass(GateArgs a, int j, uint64_t q
     }
     const uint64_t *t = m61::block_sum_lds<3 * R>(acc, red);
     if (threadIdx.x < 3 * R)
-        a.part[(size_t)(3 * j + threadIdx.x) * kGateMaxBlocks + blockIdx.x] = t[threadIdx.x];
+        a.part[(size_t)(3 * j + threadIdx.x) * kGateMaxBlocks + blk] = t[threadIdx.x];
+}
+
+template <int R>
+__global__ __launch_bounds__(256) void k_gate_pass(GateArgs a, int j, uint64_t q)
+{
+    __shared__ uint64_t red[m61::block_sum_words(3 * R, kThreads)];
+    gate_pass_block<R, false>(a, j, q, blockIdx.x, gridDim.x, red);
+}
+
+// The first pass and the product (with the witness) side by side: the one
+// works on its field products, the other waits on memory.
+template <int R, int V, bool WIT>
+__global__ __launch_bounds__(256) void k_gate_main(GateArgs a, uint64_t q, int npass, int64_t *C, WitEpi we, int nent)
+{
+    constexpr int W = m61::block_sum_words(3 * R, kThreads);
+    __shared__ uint64_t red[W > entries_lds_words(kThreads) ? W : entries_lds_words(kThreads)];
+    const int b = blockIdx.x, both = 2 * (npass < nent ? npass : nent);
+    const bool pass = b < both ? (b & 1) == 0 : npass > nent;  // workgroup-uniform
+    const int idx = b < both ? b >> 1 : b - both / 2;
+    if (pass) gate_pass_block<R, true>(a, 0, q, idx, npass, red);
+    else entries_block<V, WIT, kThreads>(GateProduct<V>{a.A, a.B}, 1ull << (a.lN - a.lk), a.lk, C, we, idx, nent, red);
 }
 
 // Round j's value at X from its sums g = (Z_0, Z_1, U).
@@ -104,11 +150,18 @@ __device__ __forceinline__ uint64_t gate_round_eval(const uint64_t *g, uint64_t 
 // j0 sums its pass's partials; a later one folds the tables the passes left (the
 // factors themselves when j0 = 0; at most 2^kGateTailLog entries) in LDS up to
 // its round and takes its sums.
-__global__ __launch_bounds__(kGateTailThreads) void k_gate_tails(GateArgs a, int j0)
+// Without passes (j0 = 0) further workgroups compute the product (ENT).
+template <bool ENT, int V, bool WIT>
+__global__ __launch_bounds__(kGateTailThreads) void k_gate_tails(GateArgs a, int j0, int64_t *C, WitEpi we)
 {
     __shared__ uint64_t t0[1 << kGateTailLog], t1[1 << kGateTailLog];
     __shared__ uint64_t red[m61::block_sum_words(3, kGateTailThreads)];
     const int j = blockIdx.x, tid = threadIdx.x;
+    if (ENT && j > a.lN) {  // workgroup-uniform
+        entries_block<V, WIT, kGateTailThreads>(GateProduct<V>{a.A, a.B}, 1ull << (a.lN - a.lk), a.lk, C, we,
+                                                j - a.lN - 1, (int)gridDim.x - a.lN - 1, red);
+        return;
+    }
     uint64_t g[3] = {0, 0, 0};
     if (j < j0) {
         const int s = j - j % kGatePass, nb = gate_blocks(1ull << (a.lN - s - gate_pass_rounds(j0 - s)));
@@ -152,29 +205,54 @@ __global__ __launch_bounds__(kGateTailThreads) void k_gate_tails(GateArgs a, int
         a.tr[0] = m61::add(gate_round_eval(t, a.K[0], a.r[0], 0), gate_round_eval(t, a.K[0], a.r[0], 1));
 }
 
-template <int R> static void gate_pass(const GateArgs &a, int j, hipStream_t st)
+int gate_entries(uint64_t N, uint64_t k, const int64_t *C, const WitEpi *we)
 {
-    const uint64_t q = 1ull << (a.lN - j - R);
-    const dim3 grid(gate_blocks(q)), blk(kThreads);
-    if (j == 0) hipLaunchKernelGGL((k_gate_pass<R, true>), grid, blk, 0, st, a, j, q);
-    else hipLaunchKernelGGL((k_gate_pass<R, false>), grid, blk, 0, st, a, j, q);
+    return entries_blocks(N, entries_width(k, C, we), N > 1ull << kGateTailLog ? kThreads : kGateTailThreads);
 }
 
-void launch_gate(const GateArgs &a, int64_t *C, hipStream_t st)
+void launch_gate(const GateArgs &a, uint64_t *E1, uint64_t *E2, int64_t *C, const WitEpi *we, hipStream_t st)
 {
-    const uint64_t N = 1ull << a.lN;
+    const uint64_t N = 1ull << a.lN, k = 1ull << a.lk;
     const XSetupArgs xs{a.r, a.rho, nullptr, a.lN, a.L, a.nhs, a.HS, a.LS, a.K, nullptr, nullptr, 0, 0};
-    hipLaunchKernelGGL(k_gate_setup, dim3((x_setup_count(xs) + kThreads - 1) / kThreads), dim3(kThreads), 0, st, xs);
-    hipLaunchKernelGGL(k_gate_product, dim3((unsigned)std::min<uint64_t>((N + kThreads - 1) / kThreads, 4096)),
-                       dim3(kThreads), 0, st, a.A, a.B, N, a.lk, C);
+    const int nx = (x_setup_count(xs) + kThreads - 1) / kThreads;
+    const unsigned ne = (unsigned)((N / k + k + kThreads - 1) / kThreads);
+    hipLaunchKernelGGL(k_gate_setup, dim3(nx + ne), dim3(kThreads), 0, st, xs, nx * kThreads, a.lN - a.lk, E1, E2);
+    const int V = entries_width(k, C, we), nent = gate_entries(N, k, C, we);
+    const WitEpi w = we ? *we : WitEpi{};
     const int j0 = a.lN > kGateTailLog ? a.lN - kGateTailLog : 0;  // rounds over the global tables
+    if (j0 == 0) {
+        const dim3 grid(a.lN + 1 + nent), blk(kGateTailThreads);
+        if (V == 2 && we) hipLaunchKernelGGL((k_gate_tails<true, 2, true>), grid, blk, 0, st, a, 0, C, w);
+        else if (V == 2) hipLaunchKernelGGL((k_gate_tails<true, 2, false>), grid, blk, 0, st, a, 0, C, w);
+        else if (we) hipLaunchKernelGGL((k_gate_tails<true, 1, true>), grid, blk, 0, st, a, 0, C, w);
+        else hipLaunchKernelGGL((k_gate_tails<true, 1, false>), grid, blk, 0, st, a, 0, C, w);
+        return;
+    }
     for (int j = 0; j < j0; j += kGatePass) {
         const int r = gate_pass_rounds(j0 - j);
-        if (r == 3) gate_pass<3>(a, j, st);
-        else if (r == 2) gate_pass<2>(a, j, st);
-        else gate_pass<1>(a, j, st);
+        const uint64_t q = 1ull << (a.lN - j - r);
+        const int nb = gate_blocks(q);
+        if (j > 0) {
+            const dim3 grid(nb), blk(kThreads);
+            if (r == 3) hipLaunchKernelGGL(k_gate_pass<3>, grid, blk, 0, st, a, j, q);
+            else if (r == 2) hipLaunchKernelGGL(k_gate_pass<2>, grid, blk, 0, st, a, j, q);
+            else hipLaunchKernelGGL(k_gate_pass<1>, grid, blk, 0, st, a, j, q);
+            continue;
+        }
+        const dim3 grid(nb + nent), blk(kThreads);
+#define RA_GATE_MAIN(R)                                                                                              \
+    do {                                                                                                             \
+        if (V == 2 && we) hipLaunchKernelGGL((k_gate_main<R, 2, true>), grid, blk, 0, st, a, q, nb, C, w, nent);      \
+        else if (V == 2) hipLaunchKernelGGL((k_gate_main<R, 2, false>), grid, blk, 0, st, a, q, nb, C, w, nent);      \
+        else if (we) hipLaunchKernelGGL((k_gate_main<R, 1, true>), grid, blk, 0, st, a, q, nb, C, w, nent);           \
+        else hipLaunchKernelGGL((k_gate_main<R, 1, false>), grid, blk, 0, st, a, q, nb, C, w, nent);                  \
+    } while (0)
+        if (r == 3) RA_GATE_MAIN(3);
+        else if (r == 2) RA_GATE_MAIN(2);
+        else RA_GATE_MAIN(1);
+#undef RA_GATE_MAIN
     }
-    hipLaunchKernelGGL(k_gate_tails, dim3(a.lN + 1), dim3(kGateTailThreads), 0, st, a, j0);
+    hipLaunchKernelGGL((k_gate_tails<false, 1, false>), dim3(a.lN + 1), dim3(kGateTailThreads), 0, st, a, j0, nullptr, w);
 }
 
 }  // namespace ra
