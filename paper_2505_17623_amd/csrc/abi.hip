@@ -43,6 +43,9 @@ struct ra_ctx {
     size_t acc_cap = 0;
     uint64_t r12_off = 0;  // the layer's (r1, r2): offset in the challenge stream
     bool link_ok = false;  // a layer over F_p has just been proven: its a* may be linked (ra_link_prove)
+    const int64_t *mm_of = nullptr;  // the product whose partial minima and maxima are in d_wit
+    int mm_parts = 0;
+    uint64_t refused = 0;   // challenges that a refused embedding has to give back
     bool is_matrix = true;  // the layer's product is a matrix product: its a* is a claim on its input
     sha::Transcript *d_fs = nullptr;  // the Fiat-Shamir transcript (ra_ctx_create_fs), on the device
     size_t eq_cap = 0;
@@ -324,6 +327,17 @@ ra_status finish(ra_ctx *c, size_t off, std::function<ra_status(const uint64_t *
     return d;
 }
 
+// A refused embedding found at a wait of its own layer gives its challenges
+// back and leaves the context between layers.
+void take_back(ra_ctx *c)
+{
+    if (!c->refused) return;
+    c->cursor -= c->refused;
+    c->refused = 0;
+    c->phase = 0;
+    c->mm_of = nullptr;
+}
+
 // Plane count of the bit table for given s, t, relu (the rule of the witness
 // kernel, Sec. III-A-2 and III-B): s + (t + 2) (1 + relu) planes, rounded up to
 // a power of two.
@@ -355,14 +369,12 @@ int log2_tail() { return log2u(tail_capacity(0)); }
 // sum_out >= 0 the claimed sum to tr[sum_out].  With tail_out given, the
 // tail is not launched: its arguments and jobs go to tail_out / jobs_out for
 // a launch that carries it as extra workgroups.
-// cmax: rounds per launch (0: the kind's own).
 void run_instance(ra_ctx *c, hipStream_t st, int kind, uint64_t *t0, uint64_t *t1, uint64_t *t2, int v,
                   const uint64_t *rho, uint64_t *tr, int ev_base, int width, uint64_t *finals, int sum_out,
                   uint64_t *part, int g_rounds, int g_tail, TailArgs *tail_out = nullptr, XJobs *jobs_out = nullptr,
-                  uint64_t *acc0 = nullptr, int cmax = 0)
+                  uint64_t *acc0 = nullptr)
 {
-    const int lt = log2_tail();
-    if (cmax == 0) cmax = fused_rounds_max(kind);
+    const int cmax = fused_rounds_max(kind), lt = log2_tail();
     XJobs jobs{};
     jobs.part = part;
     jobs.stride = kPartStride;
@@ -672,6 +684,7 @@ ra_status ra_ctx_sync(ra_ctx *c)
     const ra_status r = drain(c);
     ra_status first = c->deferred_err != RA_OK ? c->deferred_err : r;
     c->deferred_err = RA_OK;
+    c->refused = 0;  // the layers after a refused one are enqueued already
     return first;
 }
 
@@ -824,6 +837,7 @@ ra_status ra_sumcheck_matmul_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype,
     c->phase = 1;
     c->link_ok = false;
     c->is_matrix = true;
+    c->mm_of = nullptr;
     c->cursor += need;
     return finish(c, o_tr, [out, lm](const uint64_t *h) {
         out->log_m = (uint32_t)lm;
@@ -920,8 +934,10 @@ ra_status ra_rescale_relu_witness(ra_ctx *c, const int64_t *d_C, uint32_t n, uin
     if (!given) {
         Timed tm(c, G_WIT_MINMAX);
         launch_witness_params(d_C, N, (int)io->s, (int)io->relu, (int)io->round_mode, io->t,
-                              (int64_t *)(c->d_wit + kWitMinMax), c->d_params, c->stream);
+                              (int64_t *)(c->d_wit + kWitMinMax), c->d_params, c->stream, nullptr,
+                              d_C == c->mm_of ? c->mm_parts : 0);
     }
+    c->mm_of = nullptr;
     if (!planned) {   // A call that does not wait (deferred, t given) leaves its last step, the
         // sum of the claims, to the range call that must follow (its set-up
         // launch), or to the next wait on the context.
@@ -942,7 +958,7 @@ ra_status ra_rescale_relu_witness(ra_ctx *c, const int64_t *d_C, uint32_t n, uin
         io->rm_claim = h[9];
         io->y_claim = h[10];
         io->z_claim = h[11];
-        if (!known) {  // the layer state advances once t and P are known
+        if (!known && !c->refused) {  // the layer state advances once t and P are known
             c->s = (int)io->s;
             c->relu = (int)io->relu;
             c->mode = (int)io->round_mode;
@@ -966,6 +982,7 @@ ra_status ra_rescale_relu_witness(ra_ctx *c, const int64_t *d_C, uint32_t n, uin
     c->deferred = false;  // this call must wait for t and P
     st = finish(c, o_st, fill);
     c->deferred = was;
+    take_back(c);
     return st;
 }
 
@@ -1685,43 +1702,48 @@ GateLayout gate_layout(uint64_t N)
     l.o_k = cv.take<uint64_t>(lN + 1);
     l.o_t0 = cv.take<uint64_t>(std::max<uint64_t>(N / 2, 1));
     l.o_t1 = cv.take<uint64_t>(std::max<uint64_t>(N / 2, 1));
-    l.o_part = cv.take<uint64_t>((size_t)std::max(3 * lN, 1) * kGateMaxBlocks);
+    l.o_part = cv.take<uint64_t>((size_t)std::max(3 * lN, 1) * kEntryMaxBlocks);
     l.bytes = cv.off;
     return l;
 }
 
-constexpr uint32_t kEmbedMaxVocab = 1u << 22;  // the rounds' partials fit the tail's job list
+constexpr uint32_t kEmbedMaxVocab = 1u << 22;
 constexpr uint32_t kEmbedMaxWidth = 1u << 17;  // exact int32 sums of a quarter row's byte products
 struct EmbedLayout {
-    size_t o_b, o_a, o_part, o_limbs, bytes;
+    size_t o_w, o_b, o_t0, o_t1, o_part, o_limbs, bytes;
 };
 EmbedLayout embed_layout(uint64_t rows, uint32_t d)
 {
     EmbedLayout l;
     Carve cv;
+    l.o_w = cv.take<uint64_t>(2 * rows);
     l.o_b = cv.take<uint64_t>(rows);
-    l.o_a = cv.take<uint64_t>(rows);
-    l.o_part = cv.take<uint64_t>((size_t)std::max(1, log2u(rows)) * kPartStride);
+    l.o_t0 = cv.take<uint64_t>(std::max<uint64_t>(rows / 2, 1));
+    l.o_t1 = cv.take<uint64_t>(std::max<uint64_t>(rows / 2, 1));
+    l.o_part = cv.take<uint64_t>((size_t)std::max(3 * log2u(rows), 1) * kEntryMaxBlocks);
     l.o_limbs = cv.take<uint64_t>(embed_limb_words(d));
     l.bytes = cv.off;
     return l;
 }
 
-// The announced witness (ra_witness_plan) of a product computed entry by entry:
-// whether the product's launch takes it.
-bool plan_witness(ra_ctx *c, uint64_t N, uint64_t *E1, uint64_t *E2, WitEpi *we)
+// The product's outputs: C and the announced witness (ra_witness_plan), or
+// without one the partial minima and maxima that the witness call takes up.
+EntriesArgs entries_args(ra_ctx *c, uint64_t N, int64_t *d_C)
 {
+    EntriesArgs e{};
+    e.C = d_C;
+    e.mm = (int64_t *)(c->d_wit + kWitMinMax);
     const auto &pl = c->plan;
-    if (!pl.valid || pl.bits_words < N) return false;
-    *we = WitEpi{(int)pl.s, pl.t, (int)pl.relu, pl.mode == RA_ROUND_NEAREST ? (int64_t)1 << (pl.s - 1) : 0,
-                 E1, E2, pl.R, pl.Rm, pl.Y, pl.Z, pl.bits, (uint64_t *)(c->d_wit + kWitClaims),
-                 (uint32_t *)(c->d_wit + kWitFlags)};
-    return true;
+    e.wit = pl.valid && pl.bits_words >= N;
+    if (e.wit)
+        e.we = WitEpi{(int)pl.s, pl.t, (int)pl.relu, pl.mode == RA_ROUND_NEAREST ? (int64_t)1 << (pl.s - 1) : 0,
+                      nullptr, nullptr, pl.R, pl.Rm, pl.Y, pl.Z, pl.bits, (uint64_t *)(c->d_wit + kWitClaims),
+                      (uint32_t *)(c->d_wit + kWitFlags)};
+    return e;
 }
 
-// The layer's state after its product call (fused: its witness is made, with
-// ntiles partials).
-void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need, bool fused, int ntiles)
+// The layer's state after its product call.
+void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need, const EntriesArgs &e)
 {
     c->n = n;
     c->m = 1;
@@ -1730,8 +1752,10 @@ void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need, bool fused, i
     c->phase = 1;
     c->link_ok = false;
     c->is_matrix = false;
-    c->plan.fused = fused;
-    c->plan.ntiles = (uint32_t)ntiles;
+    c->plan.fused = e.wit != 0;
+    c->plan.ntiles = (uint32_t)e.total;
+    c->mm_of = e.wit ? nullptr : e.C;
+    c->mm_parts = e.wit ? 0 : e.total;
     c->cursor += need;
 }
 }  // namespace
@@ -1784,14 +1808,15 @@ extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype,
     ga.T1 = (uint64_t *)(ws + gl.o_t1);
     ga.part = (uint64_t *)(ws + gl.o_part);
     ga.tr = c->d_stage + o_tr;
-    uint64_t *E1 = c->d_eq, *E2 = c->d_eq + n;
-    WitEpi we{};
-    const bool fused = plan_witness(c, N, E1, E2, &we);
+    ga.E1 = c->d_eq;
+    ga.E2 = c->d_eq + n;
+    EntriesArgs ea = entries_args(c, N, d_C);
+    ea.total = gate_entries(ga, ea);
     {
         Timed tm(c, G_GATE);
-        launch_gate(ga, E1, E2, d_C, fused ? &we : nullptr, c->stream);
+        launch_gate(ga, ea, c->stream);
     }
-    begin_layer(c, n, k, need, fused, gate_entries(N, k, d_C, fused ? &we : nullptr));
+    begin_layer(c, n, k, need, ea);
     return finish(c, o_tr, [out, lN](const uint64_t *h) {
         out->rounds = (uint32_t)lN;
         out->c0 = h[0];
@@ -1828,7 +1853,6 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
     ra_status st = ensure_chal(c, need);
     if (st != RA_OK) return st;
     if ((st = ensure_eq(c, (size_t)n + k)) != RA_OK) return st;
-    if ((st = ensure_acc(c, rows)) != RA_OK) return st;
     const EmbedLayout el = embed_layout(rows, d);
     char *ws = nullptr;
     if ((st = call_ws(c, d_ws, ws_bytes, el.bytes, &ws)) != RA_OK) return st;
@@ -1850,33 +1874,28 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
     ea.r = c->d_chal + c->cursor;
     ea.E1 = c->d_eq;
     ea.E2 = c->d_eq + n;
-    ea.acc = c->d_acc;
+    ea.W = (uint64_t *)(ws + el.o_w);
     ea.limbs = (uint64_t *)(ws + el.o_limbs);
     ea.b = (uint64_t *)(ws + el.o_b);
-    ea.status = tr + 3 + 3 * (size_t)lv;
-    c->h_stage[o_tr + 3 + 3 * (size_t)lv] = 0;
+    ea.rho = ea.r + ln + lk;
+    ea.lv = lv;
+    ea.T0 = (uint64_t *)(ws + el.o_t0);
+    ea.T1 = (uint64_t *)(ws + el.o_t1);
+    ea.part = (uint64_t *)(ws + el.o_part);
+    ea.tr = tr;
+    c->h_stage[o_tr + 3 + 3 * (size_t)lv] = 0;  // the tokens' status
+    EntriesArgs en = entries_args(c, (uint64_t)n << lk, d_C);
+    en.total = embed_entries(ea, en);
     {
         Timed tm(c, G_EMBED);
-        launch_embed_front(ea, c->stream);
-        launch_embed_bind(ea, c->stream);
+        launch_embed(ea, en, c->stream);
     }
-    // the rounds over the vocabulary while its tables exceed the tail, at most
-    // three a launch and evenly (2^17 entries: three rounds 7.1 us, two 4.8, four 14)
-    const int left = std::max(lv - log2_tail(), 0), nl = (left + 2) / 3, per = left ? (left + nl - 1) / nl : 1;
-    TailArgs ta{};
-    XJobs jobs{};
-    run_instance(c, c->stream, KIND_MATMUL, (uint64_t *)(ws + el.o_a), ea.b, nullptr, lv, ea.r + ln + lk, tr, 1, 3,
-                 tr + 1 + 3 * lv, 0, (uint64_t *)(ws + el.o_part), G_MM_ROUNDS, G_MM_TAIL, &ta, &jobs, c->d_acc, per);
-    WitEpi we{};
-    const uint64_t N = (uint64_t)n << lk;
-    const bool fused = plan_witness(c, N, ea.E1, ea.E2, &we);
-    {
-        Timed tm(c, G_EMBED);
-        launch_embed_product(ea, d_C, fused ? &we : nullptr, ta, jobs, c->stream);
-    }
-    begin_layer(c, n, k, need, fused, embed_entries(N, k, d_C, fused ? &we : nullptr));
-    const ra_status r = finish(c, o_tr, [out, lv](const uint64_t *h) {
-        if (h[3 + 3 * lv]) return (ra_status)RA_E_INVAL;  // a token outside [-1, vocab)
+    begin_layer(c, n, k, need, en);
+    const ra_status r = finish(c, o_tr, [c, out, lv, need](const uint64_t *h) {
+        if (h[3 + 3 * lv]) {  // a token outside [-1, vocab)
+            c->refused = need;
+            return (ra_status)RA_E_INVAL;
+        }
         out->log_m = (uint32_t)lv;
         out->c0 = h[0];
         if (lv) std::memcpy(out->evals, h + 1, 3 * (size_t)lv * 8);
@@ -1884,10 +1903,7 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
         out->b_star = h[2 + 3 * lv];
         return (ra_status)RA_OK;
     });
-    if (r != RA_OK && !c->deferred) {  // refused tokens consume nothing
-        c->cursor -= need;
-        c->phase = 0;
-    }
+    take_back(c);
     return r;
 }
 

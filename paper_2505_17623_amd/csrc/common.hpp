@@ -141,8 +141,9 @@ ChunkSum launch_bind_rows_chunks(const void *T, int dtype, uint32_t rows, uint32
 void launch_bind_cols(const void *T, int dtype, uint32_t rows, uint32_t cols, const uint64_t *E, uint64_t *out,
                       hipStream_t st, const ChunkSum *cs = nullptr);
 int witness_blocks(uint64_t N);
+// made (> 0): the smallest and largest entry of C are in mm_part already, that many partials
 void launch_witness_params(const int64_t *C, uint64_t N, int s, int relu, int mode, int t_in, int64_t *mm_part,
-                           WitParams *params, hipStream_t st, WitParams *mirror = nullptr);
+                           WitParams *params, hipStream_t st, WitParams *mirror = nullptr, int made = 0);
 // mirror (optional): 12 words, the parameters (words 0-7) and the claims (8-11).
 // known (optional): parameters computed on the host for a given t (status 0);
 // then no params pass runs before, the range of R is checked here (flags:
@@ -483,17 +484,39 @@ struct LinkArgs {
 void launch_link(const LinkArgs &a, hipStream_t st);
 void launch_link_gather(const int32_t *Z, uint64_t nz, const int32_t *src, uint64_t na, int32_t *A, hipStream_t st);
 
-// ---- the gated product (gate.hip) ----
-constexpr int kGateMaxBlocks = 512;    // blocks of a pass (partials per round)
-constexpr int kGateTailLog = 11;       // the last rounds, over at most 2^11 entries, run from LDS
-constexpr int kGateTailThreads = 512;
-constexpr int kGatePass = 3;           // rounds per pass; the last pass takes what is left
-__host__ __device__ inline int gate_pass_rounds(int left) { return left < kGatePass ? left : kGatePass; }
-__host__ __device__ inline int gate_blocks(uint64_t h)
+// ---- products computed entry by entry (entries.hpp) ----
+// The product's `total` workgroups.  With wit the announced witness
+// (ra_witness_plan) in their partials (we), else each one's smallest and
+// largest entry (mm, two words).
+struct EntriesArgs {
+    int64_t *C;
+    WitEpi we;
+    int wit;
+    int64_t *mm;
+    int total;
+};
+// Rounds of an instance of v variables before its last ones: passes of at most
+// kEntryPass rounds, until at most 2^kEntryTailMax entries are left, or 2^kEntryTailLog
+// where that takes no further pass (the last rounds' time grows with them).
+constexpr int kEntryPass = 3, kEntryTailLog = 11, kEntryTailMax = 13;
+constexpr int kEntryTailThreads = 512;
+constexpr int kEntryMaxBlocks = 512;   // blocks of a pass (partials per round)
+__host__ __device__ inline int entry_passes(int v)
+{
+    return v > kEntryTailMax ? (v - kEntryTailMax + kEntryPass - 1) / kEntryPass : 0;
+}
+__host__ __device__ inline int entry_pass_rounds(int v)  // rounds over all passes
+{
+    const int most = kEntryPass * entry_passes(v), want = v > kEntryTailLog ? v - kEntryTailLog : 0;
+    return want < most ? want : most;
+}
+__host__ __device__ inline int entry_blocks(uint64_t h)
 {
     const uint64_t b = (h + kThreads - 1) / kThreads;
-    return (int)(b < (uint64_t)kGateMaxBlocks ? (b ? b : 1) : kGateMaxBlocks);
+    return (int)(b < (uint64_t)kEntryMaxBlocks ? (b ? b : 1) : kEntryMaxBlocks);
 }
+
+// ---- the gated product (gate.hip) ----
 struct GateSrc {
     const void *p;
     uint64_t ld;               // entries from row to row (0: one row for all)
@@ -503,16 +526,15 @@ struct GateArgs {
     GateSrc A, B;              // 2^lN entries, 2^lk columns
     int lN, lk;
     const uint64_t *r, *rho;   // (r1, r2) and the rounds' challenges, lN each
+    uint64_t *E1, *E2;         // out: the eq tables of r1 and r2
     int L, nhs;                // split of the suffix eq tables (xsetup.hpp)
     uint64_t *HS, *LS, *K;     // nhs, 2^(L + 1) and lN + 1 words
     uint64_t *T0, *T1;         // the folded tables: 2^(lN - 1) words each at most
-    uint64_t *part;            // 3 lN x kGateMaxBlocks words
+    uint64_t *part;            // 3 lN x kEntryMaxBlocks words
     uint64_t *tr;              // out: c0, 4 lN round words, A~(rho), B~(rho)
 };
-// The eq tables E1 (r1) and E2 (r2), C and, with we (ra_witness_plan), its
-// witness in gate_entries workgroups' partials, the sum-check.
-int gate_entries(uint64_t N, uint64_t k, const int64_t *C, const WitEpi *we);
-void launch_gate(const GateArgs &a, uint64_t *E1, uint64_t *E2, int64_t *C, const WitEpi *we, hipStream_t st);
+int gate_entries(const GateArgs &a, const EntriesArgs &e);  // e.total
+void launch_gate(const GateArgs &a, const EntriesArgs &e, hipStream_t st);
 
 // ---- the token embedding (embed.hip) ----
 struct EmbedArgs {
@@ -526,19 +548,18 @@ struct EmbedArgs {
     uint64_t rows;             // vocab rounded up to a power of two
     const uint64_t *r;         // r1, r2
     uint64_t *E1, *E2;         // out: eq tables of r1 (n) and r2 (2^lk)
-    uint64_t *acc;             // 2 rows words, zero: W's sums (tail.hpp)
+    uint64_t *W;               // 2 rows words: W's sums (embed.hip)
     uint64_t *limbs;           // embed_limb_words(d) words: eq(r2, .) in bytes
     uint64_t *b;               // rows words: e(v)
-    uint64_t *status;          // set if a token is outside (host memory, cleared by the host)
-};
+    const uint64_t *rho;       // the rounds' challenges, lv = log2 rows
+    int lv;
+    uint64_t *T0, *T1;         // the folded tables: rows / 2 words each
+    uint64_t *part;            // 3 lv x kEntryMaxBlocks words
+    uint64_t *tr;              // out: c0, 3 lv round words, W~(rho), E~(rho, r2), the tokens' status
+};                             // (host memory; the host clears the status)
 inline uint32_t embed_limb_words(uint32_t d) { return (d + 31) / 32 * 64; }
-void launch_embed_front(const EmbedArgs &a, hipStream_t st);
-void launch_embed_bind(const EmbedArgs &a, hipStream_t st);
-// C and, with we (ra_witness_plan), its witness in embed_entries workgroups'
-// partials; ta, jobs: the tail of the sum-check, run beside them
-int embed_entries(uint64_t N, uint64_t k, const int64_t *C, const WitEpi *we);
-void launch_embed_product(const EmbedArgs &a, int64_t *C, const WitEpi *we, const TailArgs &ta, const XJobs &jobs,
-                          hipStream_t st);
+int embed_entries(const EmbedArgs &a, const EntriesArgs &e);  // e.total
+void launch_embed(const EmbedArgs &a, const EntriesArgs &e, hipStream_t st);
 
 // ---- launchers (planes.hip) ----
 // The Gram pass works on 16 x 16 tiles of G on and above the diagonal: 3 for

@@ -6,15 +6,15 @@
 // the lookup's transpose applied to eq(r1, .) (what a gradient of the table
 // is to the rows' gradients), and
 //     C~(r1, r2) = sum_v W(v) e(v),   e(v) = sum_j E[v, j] eq(r2, j),
-// is the matrix layer's sum-check (Eq. (4)) over the vocabulary's variables,
-// which ends in W~(rho), computable from the public tokens, and E~(rho, r2).
+// is the matrix layer's sum-check (Eq. (4)) over the vocabulary's variables. It
+// ends in W~(rho), computable from the public tokens, and E~(rho, r2).
 // Rows past the vocabulary and columns past the table's width are zero.
 #include <algorithm>
 
 #include "common.hpp"
 #include "entries.hpp"
 #include "m61.hpp"
-#include "tail.hpp"
+#include "xpair.hpp"
 #include "xsetup.hpp"
 
 namespace ra {
@@ -64,19 +64,18 @@ __device__ __forceinline__ void embed_limbs(const uint64_t *r2, int lk, uint32_t
     limbs[t] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
 }
 
-// All that depends on the challenges alone, and W's sums: nl threads write the
-// columns' fragments, the next n and 2^lk the eq tables E1 and E2, the last n
-// (one a token) add eq(r1, i) scale to W(tok[i]).  W(v) mod p is acc[v] + 2^32
-// acc[rows + v] (tail.hpp), each word a sum of values below 2^32, so no add
-// wraps and their order does not matter.  A token outside [-1, vocab) is not
-// followed; it sets *status.
-__global__ __launch_bounds__(256) void k_embed_front(EmbedArgs a, uint32_t nl, uint64_t scale)
+// All that depends on the challenges alone: nl threads write the columns'
+// fragments, the next n and 2^lk the eq tables E1 and E2; W's 2 rows words are
+// cleared by all of them.
+__global__ __launch_bounds__(256) void k_embed_front(EmbedArgs a, uint32_t nl)
 {
     __shared__ uint64_t rl[64];
     const int ln = a.ln, lk = a.lk, tid = threadIdx.x;
     if (tid < ln + lk) rl[tid] = a.r[tid];
+    const uint64_t g = (uint64_t)blockIdx.x * blockDim.x + tid;
+    for (uint64_t i = g; i < 2 * a.rows; i += (uint64_t)gridDim.x * blockDim.x) a.W[i] = 0;
     __syncthreads();
-    uint64_t i = (uint64_t)blockIdx.x * blockDim.x + tid;
+    uint64_t i = g;
     if (i < nl) {
         embed_limbs(rl + ln, lk, a.d, (uint32_t)i, (v4i *)a.limbs);
         return;
@@ -87,20 +86,24 @@ __global__ __launch_bounds__(256) void k_embed_front(EmbedArgs a, uint32_t nl, u
         return;
     }
     i -= a.n;
-    if (i < 1ull << lk) {
-        a.E2[i] = eq_suffix(rl, ln, lk, i);
-        return;
-    }
-    i -= 1ull << lk;
+    if (i < 1ull << lk) a.E2[i] = eq_suffix(rl, ln, lk, i);
+}
+
+// W's sums, one thread a token: W(v) = acc[v] + 2^32 acc[rows + v] mod p, each
+// word a sum of values below 2^32, so no add wraps (n <= 2^31) and their order
+// does not matter.  A token outside [-1, vocab) is not followed; it sets
+// *status.
+__device__ __forceinline__ void embed_scatter(const EmbedArgs &a, uint64_t *status, uint64_t scale, uint64_t i)
+{
     if (i >= a.n) return;
     const int32_t v = a.tok[i];
     if (v < 0 || (uint32_t)v >= a.vocab) {
-        if (v != -1) *a.status = 1;
+        if (v != -1) *status = 1;
         return;
     }
-    const uint64_t e = m61::mul(eq_suffix(rl, 0, ln, i), scale);
-    atomicAdd((unsigned long long *)a.acc + v, (unsigned long long)(e & 0xFFFFFFFFull));
-    atomicAdd((unsigned long long *)a.acc + a.rows + v, (unsigned long long)(e >> 32));
+    const uint64_t e = m61::mul(a.E1[i], scale);
+    atomicAdd((unsigned long long *)a.W + v, (unsigned long long)(e & 0xFFFFFFFFull));
+    atomicAdd((unsigned long long *)a.W + a.rows + v, (unsigned long long)(e >> 32));
 }
 
 // sum_{j < d} eq(r2, j) from the coordinates of r2 (lk of them): for every set
@@ -122,14 +125,22 @@ __device__ __forceinline__ uint64_t eq_prefix_sum(const uint64_t *r2, int lk, ui
 // them; U chunks' loads are issued before the first is used.  Rows may start
 // at any even address; the last chunk of a width that is no multiple of 32 is
 // read entry by entry.
+// The first ns workgroups scatter the tokens' weights.
 template <int RT, int U>
-__global__ __launch_bounds__(256) void k_embed_bind(const int16_t *__restrict__ E, uint64_t ld, uint32_t vocab, uint32_t d,
-                                                    uint64_t rows, const v4i *__restrict__ limbs,
-                                                    const uint64_t *__restrict__ r2, int lk, uint64_t *__restrict__ b)
+__global__ __launch_bounds__(256) void k_embed_bind(EmbedArgs a_, int ns, uint64_t scale)
 {
     __shared__ int32_t part[4][16 * RT][9];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, g = lane >> 4, c = lane & 15;
-    const uint64_t v0 = (uint64_t)blockIdx.x * (16 * RT);
+    if ((int)blockIdx.x < ns) {  // workgroup-uniform
+        embed_scatter(a_, a_.tr + 3 + 3 * (size_t)a_.lv, scale, (uint64_t)blockIdx.x * 256 + tid);
+        return;
+    }
+    const int16_t *__restrict__ E = a_.E;
+    const v4i *__restrict__ limbs = (const v4i *)a_.limbs;
+    const uint64_t ld = a_.ld, rows = a_.rows, *r2 = a_.r + a_.ln;
+    const uint32_t vocab = a_.vocab, d = a_.d;
+    const int lk = a_.lk;
+    const uint64_t v0 = (uint64_t)(blockIdx.x - ns) * (16 * RT);
     const uint32_t nq = d / 32;  // whole chunks
     const v4i flip{0x00800080, 0x00800080, 0x00800080, 0x00800080}, none{0, 0, 0, 0};
     const int16_t *row[RT];
@@ -186,7 +197,7 @@ __global__ __launch_bounds__(256) void k_embed_bind(const int16_t *__restrict__ 
             s = m61::fold(s + m61::rotl(m61::from_i64(x), 8 * l));
         }
     }
-    b[v0 + tid] = m61::canon(s);
+    a_.b[v0 + tid] = m61::canon(s);
 }
 
 // V entries of C: scale times the token's row, zero past d, for token -1 and
@@ -216,59 +227,212 @@ template <int V> struct EmbedRows {
     }
 };
 
-// The product (with the witness), and the sum-check's last rounds as its first
-// workgroups.
-template <int V, bool WIT>
-__global__ __launch_bounds__(256) void k_embed_product(EmbedArgs a, int64_t *C, WitEpi we, TailArgs ta, XJobs jobs,
-                                                       int ntail)
+// One pair of a round of sum_v W(v) e(v): the sums at X = 0, 1 and of the
+// differences' products, added without folding.
+__device__ __forceinline__ void embed_pair(uint64_t u0, uint64_t u1, uint64_t v0, uint64_t v1, uint64_t *g)
 {
-    __shared__ uint64_t smem[kTailSmem];
-    static_assert(kTailSmem >= entries_lds_words(kThreads), "the tail's LDS serves the product");
-    if ((int)blockIdx.x < ntail) {  // workgroup-uniform
-        tail_block<KIND_MATMUL>(ta, jobs, blockIdx.x, smem);
-        return;
-    }
-    entries_block<V, WIT, kThreads>(EmbedRows<V>{a.tok, a.E, a.ld, a.vocab, a.d, a.scale}, a.n, a.lk, C, we,
-                                    (int)blockIdx.x - ntail, (int)gridDim.x - ntail, smem);
+    g[0] += m61::lmul(u0, v0);
+    g[1] += m61::lmul(u1, v1);
+    g[2] += m61::lmul(m61::lsub(u1, u0), m61::lsub(v1, v0));
 }
 
-void launch_embed_front(const EmbedArgs &a, hipStream_t st)
+__device__ __forceinline__ uint64_t embed_weight(const EmbedArgs &a, uint64_t i)
+{
+    return m61::fold(m61::canon(a.W[i]) + m61::rotl(m61::canon(a.W[a.rows + i]), 32));
+}
+
+// R rounds j .. j + R - 1 over tables of 2^R q entries (the first pass: W and
+// e themselves): a thread holds the 2^R entries that end in entry i of the
+// folded tables.
+template <int R, bool FIRST>
+__device__ __forceinline__ void embed_pass_block(const EmbedArgs &a, int j, uint64_t q, int blk, int nblk, uint64_t *red)
+{
+    constexpr int NL = 1 << R;
+    uint64_t rho[R], acc[3 * R];
+#pragma unroll
+    for (int c = 0; c < R; c++) rho[c] = a.rho[j + c];
+#pragma unroll
+    for (int c = 0; c < 3 * R; c++) acc[c] = 0;
+    for (uint64_t i = (uint64_t)blk * kThreads + threadIdx.x; i < q; i += (uint64_t)nblk * kThreads) {
+        uint64_t u[NL], v[NL];
+#pragma unroll
+        for (int t = 0; t < NL; t++) {
+            u[t] = FIRST ? embed_weight(a, i + t * q) : a.T0[i + t * q];
+            v[t] = FIRST ? a.b[i + t * q] : a.T1[i + t * q];
+        }
+#pragma unroll
+        for (int c = 0; c < R; c++) {
+            const int h = NL >> (c + 1);
+#pragma unroll
+            for (int p = 0; p < h; p++) {
+                embed_pair(u[p], u[p + h], v[p], v[p + h], acc + 3 * c);
+                u[p] = fold(u[p], u[p + h], rho[c]);
+                v[p] = fold(v[p], v[p + h], rho[c]);
+                if ((p & 3) == 3 || p == h - 1) fold_all<3>(acc + 3 * c);
+            }
+        }
+        a.T0[i] = m61::canon(u[0]);
+        a.T1[i] = m61::canon(v[0]);
+    }
+    const uint64_t *t = m61::block_sum_lds<3 * R>(acc, red);
+    if (threadIdx.x < 3 * R)
+        a.part[(size_t)(3 * j + threadIdx.x) * kEntryMaxBlocks + blk] = t[threadIdx.x];
+}
+
+template <int V, bool WIT, int NT>
+__device__ __forceinline__ void embed_product_block(const EmbedArgs &a, const EntriesArgs &e, int idx, uint64_t *red)
+{
+    entries_block<V, WIT, NT>(EmbedRows<V>{a.tok, a.E, a.ld, a.vocab, a.d, a.scale},
+                              [&](uint64_t row) { return a.E1[row]; }, [&](uint64_t col) { return a.E2[col]; }, a.n,
+                              a.lk, e.C, e.we, e.mm, idx, e.total, red);
+}
+
+template <int R, bool FIRST>
+__global__ __launch_bounds__(256) void k_embed_pass(EmbedArgs a, int j, uint64_t q)
+{
+    __shared__ uint64_t red[m61::block_sum_words(3 * R, kThreads)];
+    embed_pass_block<R, FIRST>(a, j, q, blockIdx.x, gridDim.x, red);
+}
+
+// One workgroup per round and one for the end, blockIdx.x = lv, as
+// k_gate_tails; the further workgroups compute the product (the passes, short of
+// workgroups and waiting on memory, were no faster beside it).
+template <int V, bool WIT>
+__global__ __launch_bounds__(kEntryTailThreads) void k_embed_tails(EmbedArgs a, int j0, EntriesArgs e)
+{
+    constexpr int NT = kEntryTailThreads, S = 1 << kEntryTailLog, EM = 1 << (kEntryTailMax - kEntryTailLog);
+    constexpr int IT = S / NT;
+    __shared__ uint64_t t0[S], t1[S];
+    __shared__ uint64_t red[m61::block_sum_words(3, NT)];
+    __shared__ uint64_t rhol[32];
+    const int j = blockIdx.x, tid = threadIdx.x;
+    if (j > a.lv) {  // workgroup-uniform
+        embed_product_block<V, WIT, NT>(a, e, j - a.lv - 1, red);
+        return;
+    }
+    uint64_t g[3] = {0, 0, 0};
+    const int m = a.lv - j0, base = m < kEntryTailLog ? m : kEntryTailLog, C = m - base;  // C <= 2 rounds in registers
+    uint64_t u[IT][EM] = {}, v[IT][EM] = {};
+    if (j >= j0) {  // asked for first, as in k_gate_tails
+#pragma unroll
+        for (int it = 0; it < IT; it++)
+#pragma unroll
+            for (int t = 0; t < EM; t++) {
+                const int i = it * NT + tid;
+                if (t >= 1 << C || i >= 1 << base) continue;
+                const uint64_t x = i + ((uint64_t)t << base);
+                u[it][t] = j0 == 0 ? embed_weight(a, x) : a.T0[x];
+                v[it][t] = j0 == 0 ? a.b[x] : a.T1[x];
+            }
+    }
+    if (tid < a.lv) rhol[tid] = a.rho[tid];
+    if (j < j0) {
+        const int s = j - j % kEntryPass, r = j0 - s < kEntryPass ? j0 - s : kEntryPass;
+        const int nb = entry_blocks(1ull << (a.lv - s - r));
+        const uint64_t *p = a.part + 3 * (size_t)j * kEntryMaxBlocks;
+        for (int b = tid; b < nb; b += NT)
+            for (int q = 0; q < 3; q++) g[q] = m61::fold(g[q] + p[(size_t)q * kEntryMaxBlocks + b]);
+    } else {
+        const int jj = j - j0, n0 = 1 << base;
+        __syncthreads();
+#pragma unroll
+        for (int it = 0; it < IT; it++) {
+            const int i = it * NT + tid;
+            if (i >= n0) continue;
+#pragma unroll
+            for (int c = 0; c < kEntryTailMax - kEntryTailLog; c++) {
+                const int h = (1 << C) >> (c + 1);
+                if (c > jj || h == 0) continue;
+#pragma unroll
+                for (int p = 0; p < EM / 2; p++) {
+                    if (p >= h) continue;
+                    const uint64_t u1 = h == 2 ? u[it][p + 2] : u[it][1], v1 = h == 2 ? v[it][p + 2] : v[it][1];
+                    if (c == jj) {
+                        embed_pair(u[it][p], u1, v[it][p], v1, g);
+                        fold_all<3>(g);
+                    } else {
+                        u[it][p] = fold(u[it][p], u1, rhol[j0 + c]);
+                        v[it][p] = fold(v[it][p], v1, rhol[j0 + c]);
+                    }
+                }
+            }
+            t0[i] = u[it][0];
+            t1[i] = v[it][0];
+        }
+        __syncthreads();
+        if (jj >= C) {
+            int n = n0;
+            for (int b = j0 + C; b < j; b++) {  // an entry's two sources are read by its own thread only
+                const uint64_t z = rhol[b];
+                n >>= 1;
+                for (int i = tid; i < n; i += NT) {
+                    t0[i] = fold(t0[i], t0[i + n], z);
+                    t1[i] = fold(t1[i], t1[i + n], z);
+                }
+                __syncthreads();
+            }
+            if (j == a.lv) {
+                if (tid != 0) return;
+                const uint64_t u = m61::canon(t0[0]), v = m61::canon(t1[0]);
+                if (a.lv == 0) a.tr[0] = m61::mul(u, v);
+                a.tr[1 + 3 * (size_t)a.lv] = u;
+                a.tr[2 + 3 * (size_t)a.lv] = v;
+                return;
+            }
+            const int h = n >> 1;
+            for (int i = tid; i < h; i += NT) {
+                embed_pair(t0[i], t0[i + h], t1[i], t1[i + h], g);
+                fold_all<3>(g);
+            }
+        }
+    }
+    const uint64_t *t = m61::block_sum_lds<3>(g, red);
+    if (tid != 0) return;
+    a.tr[1 + 3 * (size_t)j] = t[0];
+    a.tr[2 + 3 * (size_t)j] = t[1];
+    // at 2: g_0 + 2 (g_1 - g_0) + 2 (differences' products)
+    a.tr[3 + 3 * (size_t)j] = m61::sub(m61::add(m61::add(t[1], t[1]), m61::add(t[2], t[2])), t[0]);
+    if (j == 0) a.tr[0] = m61::add(t[0], t[1]);
+}
+
+int embed_entries(const EmbedArgs &a, const EntriesArgs &e)
+{
+    const int V = entries_width(1ull << a.lk, e.C, e.wit ? &e.we : nullptr);
+    return entries_blocks((uint64_t)a.n << a.lk, V, kEntryTailThreads);
+}
+
+void launch_embed(const EmbedArgs &a, const EntriesArgs &e, hipStream_t st)
 {
     const uint64_t scale = a.scale < 0 ? m61::P - (uint64_t)(-(int64_t)a.scale) : (uint64_t)a.scale;
     const uint32_t nl = embed_limb_words(a.d) / 2;
-    const uint64_t threads = nl + 2 * (uint64_t)a.n + (1ull << a.lk);
-    hipLaunchKernelGGL(k_embed_front, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a, nl, scale);
-}
-
-void launch_embed_bind(const EmbedArgs &a, hipStream_t st)
-{
-    const uint64_t *r2 = a.r + a.ln;
+    const uint64_t threads = nl + (uint64_t)a.n + (1ull << a.lk);
+    hipLaunchKernelGGL(k_embed_front, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a, nl);
+    const int ns = (int)((a.n + 255) / 256);
     // 64 rows a workgroup use each fragment of the columns four times; 16 rows
     // where 64 would leave CUs without a workgroup
     if (a.rows >= 64 * 256)
-        hipLaunchKernelGGL((k_embed_bind<4, 4>), dim3((unsigned)(a.rows / 64)), dim3(256), 0, st, a.E, a.ld, a.vocab,
-                           a.d, a.rows, (const v4i *)a.limbs, r2, a.lk, a.b);
+        hipLaunchKernelGGL((k_embed_bind<4, 4>), dim3(ns + (unsigned)(a.rows / 64)), dim3(256), 0, st, a, ns, scale);
     else
-        hipLaunchKernelGGL((k_embed_bind<1, 8>), dim3((unsigned)((a.rows + 15) / 16)), dim3(256), 0, st, a.E, a.ld,
-                           a.vocab, a.d, a.rows, (const v4i *)a.limbs, r2, a.lk, a.b);
-}
-
-int embed_entries(uint64_t N, uint64_t k, const int64_t *C, const WitEpi *we)
-{
-    return entries_blocks(N, entries_width(k, C, we), kThreads);
-}
-
-void launch_embed_product(const EmbedArgs &a, int64_t *C, const WitEpi *we, const TailArgs &ta, const XJobs &jobs,
-                          hipStream_t st)
-{
-    const uint64_t k = 1ull << a.lk;
-    const int V = entries_width(k, C, we), ntail = 1 + jobs.nslot;
-    const dim3 grid(ntail + embed_entries(a.n * k, k, C, we)), blk(kThreads);
-    const WitEpi w = we ? *we : WitEpi{};
-    if (V == 2 && we) hipLaunchKernelGGL((k_embed_product<2, true>), grid, blk, 0, st, a, C, w, ta, jobs, ntail);
-    else if (V == 2) hipLaunchKernelGGL((k_embed_product<2, false>), grid, blk, 0, st, a, C, w, ta, jobs, ntail);
-    else if (we) hipLaunchKernelGGL((k_embed_product<1, true>), grid, blk, 0, st, a, C, w, ta, jobs, ntail);
-    else hipLaunchKernelGGL((k_embed_product<1, false>), grid, blk, 0, st, a, C, w, ta, jobs, ntail);
+        hipLaunchKernelGGL((k_embed_bind<1, 8>), dim3(ns + (unsigned)((a.rows + 15) / 16)), dim3(256), 0, st, a, ns, scale);
+    const int j0 = entry_pass_rounds(a.lv);
+    for (int j = 0; j < j0; j += kEntryPass) {
+        const int r = j0 - j < kEntryPass ? j0 - j : kEntryPass;
+        const uint64_t q = 1ull << (a.lv - j - r);
+        const dim3 grid(entry_blocks(q)), blk(kThreads);
+#define RA_EMBED_PASS(R)                                                                       \
+    do {                                                                                       \
+        if (j == 0) hipLaunchKernelGGL((k_embed_pass<R, true>), grid, blk, 0, st, a, j, q);    \
+        else hipLaunchKernelGGL((k_embed_pass<R, false>), grid, blk, 0, st, a, j, q);          \
+    } while (0)
+        if (r == 3) RA_EMBED_PASS(3);
+        else if (r == 2) RA_EMBED_PASS(2);
+        else RA_EMBED_PASS(1);
+#undef RA_EMBED_PASS
+    }
+    entries_variant(1ull << a.lk, e, [&](auto V, auto W) {
+        hipLaunchKernelGGL((k_embed_tails<decltype(V)::value, decltype(W)::value>), dim3(a.lv + 1 + e.total),
+                           dim3(kEntryTailThreads), 0, st, a, j0, e);
+    });
 }
 
 }  // namespace ra

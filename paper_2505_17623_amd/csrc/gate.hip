@@ -114,7 +114,7 @@ __device__ __forceinline__ void gate_pass_block(const GateArgs &a, int j, uint64
     }
     const uint64_t *t = m61::block_sum_lds<3 * R>(acc, red);
     if (threadIdx.x < 3 * R)
-        a.part[(size_t)(3 * j + threadIdx.x) * kGateMaxBlocks + blk] = t[threadIdx.x];
+        a.part[(size_t)(3 * j + threadIdx.x) * kEntryMaxBlocks + blk] = t[threadIdx.x];
 }
 
 template <int R>
@@ -127,132 +127,219 @@ __global__ __launch_bounds__(256) void k_gate_pass(GateArgs a, int j, uint64_t q
 // The first pass and the product (with the witness) side by side: the one
 // works on its field products, the other waits on memory.
 template <int R, int V, bool WIT>
-__global__ __launch_bounds__(256) void k_gate_main(GateArgs a, uint64_t q, int npass, int64_t *C, WitEpi we, int nent)
+__global__ __launch_bounds__(256) void k_gate_first(GateArgs a, uint64_t q, int npass, EntriesArgs e)
 {
     constexpr int W = m61::block_sum_words(3 * R, kThreads);
     __shared__ uint64_t red[W > entries_lds_words(kThreads) ? W : entries_lds_words(kThreads)];
-    const int b = blockIdx.x, both = 2 * (npass < nent ? npass : nent);
-    const bool pass = b < both ? (b & 1) == 0 : npass > nent;  // workgroup-uniform
+    const int b = blockIdx.x, both = 2 * (npass < e.total ? npass : e.total);
+    const bool pass = b < both ? (b & 1) == 0 : npass > e.total;  // workgroup-uniform
     const int idx = b < both ? b >> 1 : b - both / 2;
-    if (pass) gate_pass_block<R, true>(a, 0, q, idx, npass, red);
-    else entries_block<V, WIT, kThreads>(GateProduct<V>{a.A, a.B}, 1ull << (a.lN - a.lk), a.lk, C, we, idx, nent, red);
+    if (pass) {
+        gate_pass_block<R, true>(a, 0, q, idx, npass, red);
+        return;
+    }
+    entries_block<V, WIT, kThreads>(GateProduct<V>{a.A, a.B}, [&](uint64_t row) { return a.E1[row]; },
+                                    [&](uint64_t col) { return a.E2[col]; }, 1ull << (a.lN - a.lk), a.lk, e.C, e.we,
+                                    e.mm, idx, e.total, red);
 }
 
-// Round j's value at X from its sums g = (Z_0, Z_1, U).
-__device__ __forceinline__ uint64_t gate_round_eval(const uint64_t *g, uint64_t K, uint64_t r, int X)
+// Round j's value at X from its sums g = (Z_0, Z_1, U), lin = K_j eq1(r_j, X).
+__device__ __forceinline__ uint64_t gate_round_eval(const uint64_t *g, uint64_t lin, int X)
 {
     const uint64_t f2 = m61::lsub(m61::fold(m61::fold(3 * g[0] + 4 * g[1]) + 2 * g[1]), 2 * g[2]);
     const uint64_t f = X < 2 ? g[X] : X == 2 ? f2 : m61::lmacc(g[0], 3, m61::lsub(f2, g[1]));
-    return m61::canon(m61::lmul(m61::lmul(K, eq1_at(r, X)), f));
+    return m61::canon(m61::lmul(lin, f));
 }
 
 // One workgroup per round and one for the end, blockIdx.x = lN.  A round below
 // j0 sums its pass's partials; a later one folds the tables the passes left (the
-// factors themselves when j0 = 0; at most 2^kGateTailLog entries) in LDS up to
-// its round and takes its sums.
-// Without passes (j0 = 0) further workgroups compute the product (ENT).
-template <bool ENT, int V, bool WIT>
-__global__ __launch_bounds__(kGateTailThreads) void k_gate_tails(GateArgs a, int j0, int64_t *C, WitEpi we)
+// factors themselves when j0 = 0) up to its round, the first rounds in
+// registers while more than 2^kEntryTailLog entries are left, then in LDS, and takes
+// its sums.  What it needs besides, the weights eq(r_>j, .) as the products of
+// two small tables and K_j, it makes itself.  Without passes (ALONE) the further
+// workgroups compute the product, with eq values from the point, and the
+// tables E1, E2 (nx workgroups): the call is one launch.
+template <bool ALONE, int V, bool WIT>
+__global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, int j0, EntriesArgs e)
 {
-    __shared__ uint64_t t0[1 << kGateTailLog], t1[1 << kGateTailLog];
-    __shared__ uint64_t red[m61::block_sum_words(3, kGateTailThreads)];
-    const int j = blockIdx.x, tid = threadIdx.x;
-    if (ENT && j > a.lN) {  // workgroup-uniform
-        entries_block<V, WIT, kGateTailThreads>(GateProduct<V>{a.A, a.B}, 1ull << (a.lN - a.lk), a.lk, C, we,
-                                                j - a.lN - 1, (int)gridDim.x - a.lN - 1, red);
+    constexpr int NT = kEntryTailThreads, S = 1 << kEntryTailLog, EM = 1 << (kEntryTailMax - kEntryTailLog), FH = 64;
+    constexpr int IT = S / NT;
+    __shared__ uint64_t t0[S], t1[S];
+    __shared__ uint64_t red[m61::block_sum_words(3, NT)];
+    __shared__ uint64_t rl[32], rhol[32], H[FH], Lw[FH], Kj;
+    const int j = blockIdx.x, tid = threadIdx.x, ln = a.lN - a.lk;
+    if (j > a.lN) {  // workgroup-uniform
+        const int b = j - a.lN - 1;
+        const GateProduct<V> load{a.A, a.B};
+        if constexpr (ALONE) {
+            if (tid < a.lN) rl[tid] = a.r[tid];
+            __syncthreads();
+            if (b >= e.total) {
+                const uint64_t n = 1ull << ln, k = 1ull << a.lk, step = (uint64_t)(gridDim.x - a.lN - 1 - e.total) * NT;
+                for (uint64_t i = (uint64_t)(b - e.total) * NT + tid; i < n + k; i += step) {
+                    if (i < n) a.E1[i] = eq_suffix(rl, 0, ln, i);
+                    else a.E2[i - n] = eq_suffix(rl, ln, a.lk, i - n);
+                }
+                return;
+            }
+            entries_block<V, WIT, NT>(load, [&](uint64_t row) { return eq_suffix(rl, 0, ln, row); },
+                                      [&](uint64_t col) { return eq_suffix(rl, ln, a.lk, col); }, 1ull << ln, a.lk,
+                                      e.C, e.we, e.mm, b, e.total, red);
+        }
         return;
     }
     uint64_t g[3] = {0, 0, 0};
+    const int m = a.lN - j0, base = m < kEntryTailLog ? m : kEntryTailLog, C = m - base;  // C <= 2 rounds in registers
+    const int nvar = a.lN - j - 1, lo = nvar / 2, hi = nvar - lo;  // of the weights (j >= j0: at most 12)
+    // the tables' entries (or a pass's partials) are asked for first, and land
+    // while the point, the weights and K_j are made
+    uint64_t u[IT][EM] = {}, v[IT][EM] = {};
+    if (j >= j0) {
+#pragma unroll
+        for (int it = 0; it < IT; it++)
+#pragma unroll
+            for (int t = 0; t < EM; t++) {
+                const int i = it * NT + tid;
+                if (t >= 1 << C || i >= 1 << base) continue;
+                const uint64_t x = i + ((uint64_t)t << base);
+                u[it][t] = j0 == 0 ? (uint64_t)(int64_t)gate_load(a.A, x, a.lk) : a.T0[x];
+                v[it][t] = j0 == 0 ? (uint64_t)(int64_t)gate_load(a.B, x, a.lk) : a.T1[x];
+            }
+    }
+    if (tid < a.lN) {
+        rl[tid] = a.r[tid];
+        rhol[tid] = a.rho[tid];
+    }
+    __syncthreads();
+    if (tid < 64) {  // K_j: a prefix product over the first wave (lN < 64)
+        uint64_t k = 1;
+        if (tid < j && j < a.lN) k = m61::mul(eq1_at(rl[tid], 0), m61::sub(1, rhol[tid]));
+        if (tid < j && j < a.lN) k = m61::add(m61::canon(k), m61::mul(rl[tid], rhol[tid]));
+        k = m61::wave_prefix_mul(k);
+        if (tid == 63) Kj = k;
+    }
+    if (j >= j0 && j < a.lN) {
+        if (tid >= 64 && tid - 64 < 1 << hi) H[tid - 64] = eq_suffix(rl, j + 1, hi, tid - 64);
+        if (tid >= 128 && tid - 128 < 1 << lo) Lw[tid - 128] = eq_suffix(rl, j + 1 + hi, lo, tid - 128);
+    }
+    __syncthreads();
     if (j < j0) {
-        const int s = j - j % kGatePass, nb = gate_blocks(1ull << (a.lN - s - gate_pass_rounds(j0 - s)));
-        const uint64_t *p = a.part + 3 * (size_t)j * kGateMaxBlocks;
-        for (int b = tid; b < nb; b += blockDim.x)
-            for (int q = 0; q < 3; q++) g[q] = m61::fold(g[q] + p[(size_t)q * kGateMaxBlocks + b]);
+        const int s = j - j % kEntryPass, r = j0 - s < kEntryPass ? j0 - s : kEntryPass;
+        const int nb = entry_blocks(1ull << (a.lN - s - r));
+        const uint64_t *p = a.part + 3 * (size_t)j * kEntryMaxBlocks;
+        for (int b = tid; b < nb; b += NT)
+            for (int q = 0; q < 3; q++) g[q] = m61::fold(g[q] + p[(size_t)q * kEntryMaxBlocks + b]);
     } else {
-        int n = 1 << (a.lN - j0);
-        for (int i = tid; i < n; i += blockDim.x) {
-            t0[i] = j0 == 0 ? small_to_field(gate_load(a.A, i, a.lk)) : a.T0[i];
-            t1[i] = j0 == 0 ? small_to_field(gate_load(a.B, i, a.lk)) : a.T1[i];
+        const int jj = j - j0, n0 = 1 << base;
+        auto weight = [&](int i) { return m61::lmul(H[i >> lo], Lw[i & ((1 << lo) - 1)]); };
+#pragma unroll
+        for (int it = 0; it < IT; it++) {
+            const int i = it * NT + tid;
+            if (i >= n0) continue;
+            if (j0 == 0)
+#pragma unroll
+                for (int t = 0; t < EM; t++) {
+                    u[it][t] = small_to_field((int64_t)u[it][t]);
+                    v[it][t] = small_to_field((int64_t)v[it][t]);
+                }
+#pragma unroll
+            for (int c = 0; c < kEntryTailMax - kEntryTailLog; c++) {
+                const int h = (1 << C) >> (c + 1);
+                if (c > jj || h == 0) continue;
+#pragma unroll
+                for (int p = 0; p < EM / 2; p++) {
+                    if (p >= h) continue;
+                    const uint64_t u1 = h == 2 ? u[it][p + 2] : u[it][1], v1 = h == 2 ? v[it][p + 2] : v[it][1];
+                    if (c == jj) {
+                        relu_pair(weight(p * n0 + i), u[it][p], u1, v[it][p], v1, g);
+                        fold_all<3>(g);
+                    } else {
+                        u[it][p] = fold(u[it][p], u1, rhol[j0 + c]);
+                        v[it][p] = fold(v[it][p], v1, rhol[j0 + c]);
+                    }
+                }
+            }
+            t0[i] = u[it][0];
+            t1[i] = v[it][0];
         }
         __syncthreads();
-        for (int b = j0; b < j; b++) {  // an entry's two sources are read by its own thread only
-            const uint64_t z = a.rho[b];
-            n >>= 1;
-            for (int i = tid; i < n; i += blockDim.x) {
-                t0[i] = fold(t0[i], t0[i + n], z);
-                t1[i] = fold(t1[i], t1[i + n], z);
+        if (jj >= C) {
+            int n = n0;
+            for (int b = j0 + C; b < j; b++) {  // an entry's two sources are read by its own thread only
+                const uint64_t z = rhol[b];
+                n >>= 1;
+                for (int i = tid; i < n; i += NT) {
+                    t0[i] = fold(t0[i], t0[i + n], z);
+                    t1[i] = fold(t1[i], t1[i + n], z);
+                }
+                __syncthreads();
             }
-            __syncthreads();
-        }
-        if (j == a.lN) {
-            if (tid != 0) return;
-            const uint64_t u = m61::canon(t0[0]), v = m61::canon(t1[0]);
-            if (a.lN == 0) a.tr[0] = m61::mul(u, v);
-            a.tr[1 + 4 * (size_t)a.lN] = u;
-            a.tr[2 + 4 * (size_t)a.lN] = v;
-            return;
-        }
-        const int h = n >> 1;
-        for (int i = tid; i < h; i += blockDim.x) {
-            relu_pair(a.LS[h + i], t0[i], t0[i + h], t1[i], t1[i + h], g);
-            fold_all<3>(g);
+            if (j == a.lN) {
+                if (tid != 0) return;
+                const uint64_t u = m61::canon(t0[0]), v = m61::canon(t1[0]);
+                if (a.lN == 0) a.tr[0] = m61::mul(u, v);
+                a.tr[1 + 4 * (size_t)a.lN] = u;
+                a.tr[2 + 4 * (size_t)a.lN] = v;
+                return;
+            }
+            const int h = n >> 1;
+            for (int i = tid; i < h; i += NT) {
+                relu_pair(weight(i), t0[i], t0[i + h], t1[i], t1[i + h], g);
+                fold_all<3>(g);
+            }
         }
     }
+    const uint64_t lin = m61::lmul(Kj, eq1_at(rl[j], tid & 3));
     const uint64_t *t = m61::block_sum_lds<3>(g, red);
     if (tid >= 4) return;
-    a.tr[1 + 4 * (size_t)j + tid] = gate_round_eval(t, a.K[j], a.r[j], tid);
-    if (j == 0 && tid == 0)
-        a.tr[0] = m61::add(gate_round_eval(t, a.K[0], a.r[0], 0), gate_round_eval(t, a.K[0], a.r[0], 1));
+    const uint64_t val = gate_round_eval(t, lin, tid), next = __shfl_down(val, 1, 64);
+    a.tr[1 + 4 * (size_t)j + tid] = val;
+    if (j == 0 && tid == 0) a.tr[0] = m61::add(val, next);  // the claimed sum g_1(0) + g_1(1)
 }
 
-int gate_entries(uint64_t N, uint64_t k, const int64_t *C, const WitEpi *we)
+int gate_entries(const GateArgs &a, const EntriesArgs &e)
 {
-    return entries_blocks(N, entries_width(k, C, we), N > 1ull << kGateTailLog ? kThreads : kGateTailThreads);
+    const int V = entries_width(1ull << a.lk, e.C, e.wit ? &e.we : nullptr);
+    return entries_blocks(1ull << a.lN, V, entry_passes(a.lN) ? kThreads : kEntryTailThreads);
 }
 
-void launch_gate(const GateArgs &a, uint64_t *E1, uint64_t *E2, int64_t *C, const WitEpi *we, hipStream_t st)
+void launch_gate(const GateArgs &a, const EntriesArgs &e, hipStream_t st)
 {
-    const uint64_t N = 1ull << a.lN, k = 1ull << a.lk;
-    const XSetupArgs xs{a.r, a.rho, nullptr, a.lN, a.L, a.nhs, a.HS, a.LS, a.K, nullptr, nullptr, 0, 0};
-    const int nx = (x_setup_count(xs) + kThreads - 1) / kThreads;
-    const unsigned ne = (unsigned)((N / k + k + kThreads - 1) / kThreads);
-    hipLaunchKernelGGL(k_gate_setup, dim3(nx + ne), dim3(kThreads), 0, st, xs, nx * kThreads, a.lN - a.lk, E1, E2);
-    const int V = entries_width(k, C, we), nent = gate_entries(N, k, C, we);
-    const WitEpi w = we ? *we : WitEpi{};
-    const int j0 = a.lN > kGateTailLog ? a.lN - kGateTailLog : 0;  // rounds over the global tables
-    if (j0 == 0) {
-        const dim3 grid(a.lN + 1 + nent), blk(kGateTailThreads);
-        if (V == 2 && we) hipLaunchKernelGGL((k_gate_tails<true, 2, true>), grid, blk, 0, st, a, 0, C, w);
-        else if (V == 2) hipLaunchKernelGGL((k_gate_tails<true, 2, false>), grid, blk, 0, st, a, 0, C, w);
-        else if (we) hipLaunchKernelGGL((k_gate_tails<true, 1, true>), grid, blk, 0, st, a, 0, C, w);
-        else hipLaunchKernelGGL((k_gate_tails<true, 1, false>), grid, blk, 0, st, a, 0, C, w);
+    const int np = entry_passes(a.lN), j0 = entry_pass_rounds(a.lN);
+    const uint64_t tables = (1ull << (a.lN - a.lk)) + (1ull << a.lk);  // entries of E1 and E2
+    const dim3 tail(kEntryTailThreads);
+    if (np == 0) {
+        const unsigned nx = (unsigned)((tables + kEntryTailThreads - 1) / kEntryTailThreads);
+        entries_variant(1ull << a.lk, e, [&](auto V, auto W) {
+            hipLaunchKernelGGL((k_gate_tails<true, decltype(V)::value, decltype(W)::value>),
+                               dim3(a.lN + 1 + e.total + nx), tail, 0, st, a, 0, e);
+        });
         return;
     }
-    for (int j = 0; j < j0; j += kGatePass) {
-        const int r = gate_pass_rounds(j0 - j);
+    const XSetupArgs xs{a.r, a.rho, nullptr, a.lN, a.L, a.nhs, a.HS, a.LS, a.K, nullptr, nullptr, 0, 0};
+    const int nx = (x_setup_count(xs) + kThreads - 1) / kThreads;
+    const unsigned ne = (unsigned)((tables + kThreads - 1) / kThreads);
+    hipLaunchKernelGGL(k_gate_setup, dim3(nx + ne), dim3(kThreads), 0, st, xs, nx * kThreads, a.lN - a.lk, a.E1, a.E2);
+    for (int p = 0, j = 0; p < np; p++) {
+        const int r = j0 - j < kEntryPass ? j0 - j : kEntryPass;
         const uint64_t q = 1ull << (a.lN - j - r);
-        const int nb = gate_blocks(q);
-        if (j > 0) {
-            const dim3 grid(nb), blk(kThreads);
-            if (r == 3) hipLaunchKernelGGL(k_gate_pass<3>, grid, blk, 0, st, a, j, q);
-            else if (r == 2) hipLaunchKernelGGL(k_gate_pass<2>, grid, blk, 0, st, a, j, q);
-            else hipLaunchKernelGGL(k_gate_pass<1>, grid, blk, 0, st, a, j, q);
-            continue;
-        }
-        const dim3 grid(nb + nent), blk(kThreads);
-#define RA_GATE_MAIN(R)                                                                                              \
-    do {                                                                                                             \
-        if (V == 2 && we) hipLaunchKernelGGL((k_gate_main<R, 2, true>), grid, blk, 0, st, a, q, nb, C, w, nent);      \
-        else if (V == 2) hipLaunchKernelGGL((k_gate_main<R, 2, false>), grid, blk, 0, st, a, q, nb, C, w, nent);      \
-        else if (we) hipLaunchKernelGGL((k_gate_main<R, 1, true>), grid, blk, 0, st, a, q, nb, C, w, nent);           \
-        else hipLaunchKernelGGL((k_gate_main<R, 1, false>), grid, blk, 0, st, a, q, nb, C, w, nent);                  \
-    } while (0)
-        if (r == 3) RA_GATE_MAIN(3);
-        else if (r == 2) RA_GATE_MAIN(2);
-        else RA_GATE_MAIN(1);
-#undef RA_GATE_MAIN
+        const int nb = entry_blocks(q);
+        const dim3 blk(kThreads);
+        if (p == 0) {
+            entries_variant(1ull << a.lk, e, [&](auto Vc, auto Wc) {
+                constexpr int V = decltype(Vc)::value;
+                constexpr bool W = decltype(Wc)::value;
+                const dim3 grid(nb + e.total);
+                if (r == 3) hipLaunchKernelGGL((k_gate_first<3, V, W>), grid, blk, 0, st, a, q, nb, e);
+                else if (r == 2) hipLaunchKernelGGL((k_gate_first<2, V, W>), grid, blk, 0, st, a, q, nb, e);
+                else hipLaunchKernelGGL((k_gate_first<1, V, W>), grid, blk, 0, st, a, q, nb, e);
+            });
+        } else if (r == 3) hipLaunchKernelGGL(k_gate_pass<3>, dim3(nb), blk, 0, st, a, j, q);
+        else if (r == 2) hipLaunchKernelGGL(k_gate_pass<2>, dim3(nb), blk, 0, st, a, j, q);
+        else hipLaunchKernelGGL(k_gate_pass<1>, dim3(nb), blk, 0, st, a, j, q);
+        j += r;
     }
-    hipLaunchKernelGGL((k_gate_tails<false, 1, false>), dim3(a.lN + 1), dim3(kGateTailThreads), 0, st, a, j0, nullptr, w);
+    hipLaunchKernelGGL((k_gate_tails<false, 1, false>), dim3(a.lN + 1), tail, 0, st, a, j0, e);
 }
 
 }  // namespace ra

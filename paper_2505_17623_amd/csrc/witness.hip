@@ -608,10 +608,10 @@ void launch_claims_final(const ClaimsJob &j, hipStream_t st)
 }
 
 void launch_witness_params(const int64_t *C, uint64_t N, int s, int relu, int mode, int t_in, int64_t *mm_part,
-                           WitParams *params, hipStream_t st, WitParams *mirror)
+                           WitParams *params, hipStream_t st, WitParams *mirror, int made)
 {
-    const int nb = witness_blocks(N);
-    hipLaunchKernelGGL(k_minmax, dim3(nb), dim3(kThreads), 0, st, C, N, mm_part);
+    const int nb = made > 0 ? made : witness_blocks(N);
+    if (made <= 0) hipLaunchKernelGGL(k_minmax, dim3(nb), dim3(kThreads), 0, st, C, N, mm_part);
     hipLaunchKernelGGL(k_wit_params, dim3(1), dim3(256), 0, st, (const int64_t *)mm_part, nb, s, relu, mode, t_in,
                        params, mirror);
 }

@@ -476,32 +476,64 @@ def prove_layer(ctx: Context, A: torch.Tensor, B: torch.Tensor, s: int, relu: bo
 
 
 # --- layers with another product than a matrix's ------------------------------
-def _finish_layer(ctx: Context, C, product, s, relu, mode, t, wit, ws):
-    """The witness and range calls that end a layer after its product call."""
-    (R, Rm, Y, Z, bits), info = ra_rescale_relu_witness(ctx, C, s, relu, mode, t, wit, ws)
-    rs = ra_range_prove(ctx, bits, R, Y, info, ws)
+class _Outputs:
+    """A layer's device outputs and their pointers, kept together so that a
+    caller with kept buffers marshals them once."""
+
+    def __init__(self, n, k, device, bufs=None):
+        self.shape = (n, k)
+        if bufs is not None and "C" in bufs:
+            self.C, self.wit = bufs["C"], bufs["wit"]
+        else:
+            self.C, self.wit = torch.empty((n, k), dtype=torch.int64, device=device), witness_outputs(n, k, device)
+        assert self.C.shape == (n, k)
+        self.ptr = [_dptr(x) for x in (self.C, *self.wit)]
+        if bufs is not None:
+            bufs.update(C=self.C, wit=self.wit, outputs=self)
+
+
+def _outputs(n, k, device, bufs):
+    o = None if bufs is None else bufs.get("outputs")
+    if o is None or o.C is not bufs["C"] or o.wit is not bufs["wit"] or o.shape != (n, k):
+        o = _Outputs(n, k, device, bufs)
+    return o
+
+
+def _product_layer(ctx: Context, o: _Outputs, first, s, relu, mode, t, plan, ws):
+    """A layer's three calls, first(pC, ws) its product call, which returns a
+    function that gives its part of the transcript.  With t given the witness
+    is announced; without, the witness call waits by itself, so the product
+    call leaves its wait to that."""
+    L, (n, k), (pC, pR, pRm, pY, pZ, pbits), (pw, nw) = lib(), o.shape, o.ptr, _ws(ws)
+    relu, N = int(bool(relu)), n * k
+    join = t < 0 and not ctx.deferred
+    if t >= 0 and plan:
+        _check(L.ra_witness_plan(ctx.h, s, relu, mode, t, pR, pRm, pY, pZ, pbits, N), "ra_witness_plan")
+    info = WitnessInfo(s=s, relu=relu, round_mode=mode, t=t)
+    if join:
+        ctx.set_deferred(True)
+    try:
+        product = first(pC, pw, nw)
+        _check(L.ra_rescale_relu_witness(ctx.h, pC, n, k, pR, pRm, pY, pZ, pbits, N, pw, nw, ctypes.byref(info)),
+               "ra_rescale_relu_witness")
+    finally:
+        if join:
+            ctx.set_deferred(False)
+    lN = N.bit_length() - 1
+    rounds = info.P.bit_length() - 1 + lN
+    ev, zev, pr = (u64 * (4 * rounds))(), (u64 * max(4 * lN * relu, 1))(), RangeProof()
+    pr.evals, pr.relu_evals = ev, zev
+    _check(L.ra_range_prove(ctx.h, pbits, pR, pY, n, k, ctypes.byref(info), pw, nw, ctypes.byref(pr)), "ra_range_prove")
     tr = {}
 
     def fill():
-        tr.update(product)
-        tr.update(rs)
-        tr.update(t=int(info.t), P=int(info.P), r_claim=int(info.r_claim), rm_claim=int(info.rm_claim),
-                  y_claim=int(info.y_claim), z_claim=int(info.z_claim), s=s, relu=int(bool(relu)), mode=mode)
+        tr.update(product())
+        tr.update(rs_evals=ev[:], range_sum=pr.range_sum, bits_claim=pr.bits_claim, zc_evals=zev[:4 * pr.relu_rounds],
+                  r_at=pr.r_at, y_at=pr.y_at, t=info.t, P=info.P, r_claim=info.r_claim, rm_claim=info.rm_claim,
+                  y_claim=info.y_claim, z_claim=info.z_claim, s=s, relu=relu, mode=mode)
     ctx.later(fill)
-    return dict(C=C, R=R, Rm=Rm, Y=Y, Z=Z, bits=bits, transcript=tr)
-
-
-def _layer_outputs(ctx: Context, n, k, s, relu, mode, t, bufs, plan, device):
-    """(C, witness outputs) of a layer, kept in bufs where given; the witness
-    is announced where t is given."""
-    if bufs is not None and "C" not in bufs:
-        bufs["C"] = torch.empty((n, k), dtype=torch.int64, device=device)
-        bufs["wit"] = witness_outputs(n, k, device)
-    C, wit = (bufs["C"], bufs["wit"]) if bufs is not None else (
-        torch.empty((n, k), dtype=torch.int64, device=device), witness_outputs(n, k, device))
-    if t >= 0 and plan:
-        ra_witness_plan(ctx, s, relu, mode, t, wit)
-    return C, wit
+    R, Rm, Y, Z, bits = o.wit
+    return dict(C=o.C, R=R, Rm=Rm, Y=Y, Z=Z, bits=bits, transcript=tr)
 
 
 def _rows(T: torch.Tensor):
@@ -512,27 +544,35 @@ def _rows(T: torch.Tensor):
     return ctypes.c_void_p(T.data_ptr()), ld
 
 
+def _gate_call(ctx: Context, A, B, pC, pw, nw):
+    """The gated product's call; returns a function for its part of the transcript."""
+    n, k = A.shape
+    assert B.shape == (n, k)
+    lN = (n * k).bit_length() - 1
+    ev, pr = (u64 * max(4 * lN, 1))(), GateProof()
+    pr.evals = ev
+    (pa, lda), (pb, ldb) = _rows(A), _rows(B)
+    _check(lib().ra_gate_prove(ctx.h, pa, _DT[A.dtype], lda, pb, _DT[B.dtype], ldb, n, k, pC, pw, nw,
+                               ctypes.byref(pr)), "ra_gate_prove")
+    return lambda: dict(c0=pr.c0, gate_evals=ev[:4 * lN], a_at=pr.a_at, b_at=pr.b_at)
+
+
+def _product_output(n, k, C, device):
+    if C is None:
+        C = torch.empty((n, k), dtype=torch.int64, device=device)
+    assert C.shape == (n, k) and C.dtype == torch.int64
+    return C, _dptr(C)
+
+
 def ra_gate_prove(ctx: Context, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor | None = None,
                   ws: torch.Tensor | None = None):
     """The gated product's call (ra_gate_prove), in the matrix call's place:
     C = A * B entry by entry.  A, B: int16 or int32 n x k, rows at any stride
     (a broadcast row: stride 0).  Returns (C, dict(c0, gate_evals, a_at, b_at)),
     the dict filled at ctx.sync() in deferred mode."""
-    n, k = A.shape
-    assert B.shape == (n, k)
-    if C is None:
-        C = torch.empty((n, k), dtype=torch.int64, device=A.device)
-    assert C.shape == (n, k) and C.dtype == torch.int64 and C.is_contiguous()
-    lN = (n * k).bit_length() - 1
-    ev = np.zeros(max(4 * lN, 1), dtype=np.uint64)
-    pr = GateProof()
-    pr.evals = ev.ctypes.data_as(u64p)
-    (pa, lda), (pb, ldb) = _rows(A), _rows(B)
-    _check(lib().ra_gate_prove(ctx.h, pa, _DT[A.dtype], lda, pb, _DT[B.dtype], ldb, n, k, _dptr(C), *_ws(ws),
-                               ctypes.byref(pr)), "ra_gate_prove")
-    res = {}
-    ctx.later(lambda: res.update(c0=int(pr.c0), gate_evals=ev[:4 * lN].tolist(), a_at=int(pr.a_at),
-                                 b_at=int(pr.b_at)))
+    C, pC = _product_output(*A.shape, C, A.device)
+    product, res = _gate_call(ctx, A, B, pC, *_ws(ws)), {}
+    ctx.later(lambda: res.update(product()))
     return C, res
 
 
@@ -549,10 +589,21 @@ def prove_gate(ctx: Context, A: torch.Tensor, B: torch.Tensor, s: int, relu: boo
     other projection's output).  Arguments, buffers and results as
     prove_layer; the transcript has gate_evals, a_at, b_at in place of the
     matrix's."""
-    n, k = A.shape
-    C, wit = _layer_outputs(ctx, n, k, s, relu, mode, t, bufs, plan, A.device)
-    C, pr = ra_gate_prove(ctx, A, B, C, ws)
-    return _finish_layer(ctx, C, pr, s, relu, mode, t, wit, ws)
+    o = _outputs(*A.shape, A.device, bufs)
+    return _product_layer(ctx, o, lambda *c: _gate_call(ctx, A, B, *c), s, relu, mode, t, plan, ws)
+
+
+def _embed_call(ctx: Context, tokens, E, scale, pC, pw, nw):
+    """The token embedding's call; returns a function for its part of the transcript."""
+    assert tokens.dtype == torch.int32 and E.dtype == torch.int16
+    n, (vocab, d) = tokens.numel(), E.shape
+    lv = (vocab - 1).bit_length()
+    ev, pr = (u64 * max(3 * lv, 1))(), MatmulProof()
+    pr.evals = ev
+    pe, lde = _rows(E)
+    _check(lib().ra_embed_prove(ctx.h, _dptr(tokens), n, pe, lde, vocab, d, scale, pC, pw, nw, ctypes.byref(pr)),
+           "ra_embed_prove")
+    return lambda: dict(c0=pr.c0, mm_evals=ev[:3 * lv], a_star=pr.a_star, b_star=pr.b_star)
 
 
 def ra_embed_prove(ctx: Context, tokens: torch.Tensor, E: torch.Tensor, scale: int, C: torch.Tensor | None = None,
@@ -562,22 +613,9 @@ def ra_embed_prove(ctx: Context, tokens: torch.Tensor, E: torch.Tensor, scale: i
     with zeros to a power of two.  tokens: a power of two of int32; E: vocab x d
     int16, rows at any stride.  Returns (C, dict(c0, mm_evals, a_star, b_star)),
     the dict filled at ctx.sync() in deferred mode."""
-    assert tokens.dtype == torch.int32 and E.dtype == torch.int16
-    n, (vocab, d) = tokens.numel(), E.shape
-    k = 1 << (d - 1).bit_length()
-    if C is None:
-        C = torch.empty((n, k), dtype=torch.int64, device=E.device)
-    assert C.shape == (n, k) and C.dtype == torch.int64 and C.is_contiguous()
-    lv = (vocab - 1).bit_length()
-    ev = np.zeros(max(3 * lv, 1), dtype=np.uint64)
-    pr = MatmulProof()
-    pr.evals = ev.ctypes.data_as(u64p)
-    pe, lde = _rows(E)
-    _check(lib().ra_embed_prove(ctx.h, _dptr(tokens), n, pe, lde, vocab, d, scale, _dptr(C), *_ws(ws),
-                                ctypes.byref(pr)), "ra_embed_prove")
-    res = {}
-    ctx.later(lambda: res.update(c0=int(pr.c0), mm_evals=ev[:3 * lv].tolist(), a_star=int(pr.a_star),
-                                 b_star=int(pr.b_star)))
+    C, pC = _product_output(tokens.numel(), 1 << (E.shape[1] - 1).bit_length(), C, E.device)
+    product, res = _embed_call(ctx, tokens, E, scale, pC, *_ws(ws)), {}
+    ctx.later(lambda: res.update(product()))
     return C, res
 
 
@@ -593,10 +631,8 @@ def prove_embed(ctx: Context, tokens: torch.Tensor, E: torch.Tensor, scale: int,
     """One layer whose product is the scaled embedding of tokens, rounded by s
     bits (scale a factor with s fractional bits: Z = round(scale E[token] /
     2^s)).  Arguments, buffers and results as prove_layer."""
-    k = 1 << (E.shape[1] - 1).bit_length()
-    C, wit = _layer_outputs(ctx, tokens.numel(), k, s, relu, mode, t, bufs, plan, E.device)
-    C, pr = ra_embed_prove(ctx, tokens, E, scale, C, ws)
-    return _finish_layer(ctx, C, pr, s, relu, mode, t, wit, ws)
+    o = _outputs(tokens.numel(), 1 << (E.shape[1] - 1).bit_length(), E.device, bufs)
+    return _product_layer(ctx, o, lambda *c: _embed_call(ctx, tokens, E, scale, *c), s, relu, mode, t, plan, ws)
 
 
 def prove_gated_ffn(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, s: int,
