@@ -65,7 +65,7 @@ struct ra_ctx {
         uint64_t bits_words = 0;
         uint32_t ntiles = 0;
     } plan;
-    uint64_t *d_claims = nullptr;  // R~, Rm~, Y~, Z~ at (r1, r2)
+    uint64_t *d_claims = nullptr;  // R~, Rm~, Y~, Z~ at (r1, r2), then C~ of a product by entries
     int s = 0, relu = 0, mode = 0, t = 0, P = 0;
     // kernel-group timing (ra_ctx_set_profiling)
     bool prof_on = false;
@@ -923,7 +923,8 @@ ra_status ra_rescale_relu_witness(ra_ctx *c, const int64_t *d_C, uint32_t n, uin
                          d_Z == pl.Z && d_bits == pl.bits;
     if (planned) {
         const ClaimsJob j{(const uint64_t *)(c->d_wit + kWitClaims), (int)pl.ntiles, c->d_params, c->d_claims,
-                          c->d_stage + o_st, hp, 1, (const uint32_t *)(c->d_wit + kWitFlags)};
+                          c->d_stage + o_st, hp, 1, (const uint32_t *)(c->d_wit + kWitFlags),
+                          c->is_matrix ? nullptr : c->d_claims + 4};
         if (known) {
             c->pend_claims = j;
         } else {
@@ -1733,6 +1734,7 @@ EntriesArgs entries_args(ra_ctx *c, uint64_t N, int64_t *d_C)
     EntriesArgs e{};
     e.C = d_C;
     e.mm = (int64_t *)(c->d_wit + kWitMinMax);
+    e.c0 = c->d_claims + 4;
     const auto &pl = c->plan;
     e.wit = pl.valid && pl.bits_words >= N;
     if (e.wit)

@@ -75,6 +75,11 @@ __device__ __forceinline__ void claims_final_block(const ClaimsJob &j, uint64_t 
             for (int i = 0; i < 4; i++) acc[i] = m61::add(acc[i], j.part[4 * b + i]);
     m61::block_sum<4>(acc, red);
     if (threadIdx.x == 0) {
+        if (j.c0) {  // R~ = (C~ - Rm~ + half) / 2^s, Z~ = (R~ + Y~) / 2 under ReLU (2^61 = 1)
+            const uint64_t half = p.mode == RA_ROUND_NEAREST ? 1ull << (p.s - 1) : 0;
+            acc[0] = m61::rotl(m61::add(m61::sub(*j.c0, acc[1]), half), 61 - p.s);
+            acc[3] = p.relu ? m61::rotl(m61::add(acc[0], acc[2]), 60) : acc[0];
+        }
         if (p.status == 0)
             for (int i = 0; i < 4; i++) j.out[i] = acc[i];
         uint64_t w[12];

@@ -200,6 +200,7 @@ struct ClaimsJob {
     WitParams hp;
     int known;
     const uint32_t *flags;
+    const uint64_t *c0;  // optional: C~; then only Rm~ and Y~ are in the partials (entries.hpp)
 };
 void launch_claims_final(const ClaimsJob &j, hipStream_t st);
 // Constant block of the plane rounds (rsetup.hpp): lambda/mu/tau_p/sigma_p at
@@ -494,6 +495,7 @@ struct EntriesArgs {
     int wit;
     int64_t *mm;
     int total;
+    uint64_t *c0;              // out: C~, the sum that the product's sum-check claims
 };
 // Rounds of an instance of v variables before its last ones: passes of at most
 // kEntryPass rounds, until at most 2^kEntryTailMax entries are left, or 2^kEntryTailLog

@@ -208,37 +208,53 @@ template <int V> struct EmbedRows {
     uint64_t ld;
     uint32_t vocab, d;
     int32_t scale;
-    __device__ __forceinline__ void operator()(uint64_t row, uint64_t col, int64_t (&c)[V]) const
+    struct Raw {
+        int16_t h[V];
+    };
+    template <int U>
+    __device__ __forceinline__ void fetch(uint64_t row, uint64_t step, uint64_t col, Raw (&raw)[U]) const
     {
-        const int32_t v = tok[row];
-        int16_t h[V] = {};
-        if (v >= 0 && (uint32_t)v < vocab && col < d) {
-            const int16_t *p = E + (uint64_t)v * ld + col;
-            if (col + V <= d) {
-                __builtin_memcpy(h, p, sizeof h);
+        int32_t v[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) v[u] = tok[row + u * step];
+        const bool whole = V == 1 || !(d & 1);  // a pair of columns lies within the table's or past them
+        const uint64_t c0 = col < d ? col : 0;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int16_t *p = E + (uint64_t)((uint32_t)v[u] < vocab ? v[u] : 0) * ld + c0;  // row 0 for those outside
+            if (whole) {
+                __builtin_memcpy(raw[u].h, p, sizeof raw[u].h);
             } else {
 #pragma unroll
-                for (int i = 0; i < V; i++)
-                    if (col + i < d) h[i] = p[i];
+                for (int i = 0; i < V; i++) raw[u].h[i] = p[c0 + i < d ? i : 0];
             }
         }
 #pragma unroll
-        for (int i = 0; i < V; i++) c[i] = (int64_t)scale * h[i];
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < V; i++)
+                if ((uint32_t)v[u] >= vocab || col + i >= d) raw[u].h[i] = 0;
+    }
+    __device__ __forceinline__ void value(const Raw &r, int64_t (&c)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; i++) c[i] = (int64_t)scale * r.h[i];
     }
 };
 
-// One pair of a round of sum_v W(v) e(v): the sums at X = 0, 1 and of the
-// differences' products, added without folding.
+// One pair of a round of sum_v W(v) e(v), added to folded sums: at X = 0 and
+// 1, and the differences' products.
 __device__ __forceinline__ void embed_pair(uint64_t u0, uint64_t u1, uint64_t v0, uint64_t v1, uint64_t *g)
 {
-    g[0] += m61::lmul(u0, v0);
-    g[1] += m61::lmul(u1, v1);
-    g[2] += m61::lmul(m61::lsub(u1, u0), m61::lsub(v1, v0));
+    g[0] = m61::lmacc(g[0], u0, v0);
+    g[1] = m61::lmacc(g[1], u1, v1);
+    g[2] = m61::lmacc(g[2], m61::lsub(u1, u0), m61::lsub(v1, v0));
 }
 
-__device__ __forceinline__ uint64_t embed_weight(const EmbedArgs &a, uint64_t i)
+// W's value from its two sums.
+__device__ __forceinline__ uint64_t embed_weight(uint64_t lo, uint64_t hi)
 {
-    return m61::fold(m61::canon(a.W[i]) + m61::rotl(m61::canon(a.W[a.rows + i]), 32));
+    return m61::fold(m61::canon(lo) + m61::rotl(m61::canon(hi), 32));
 }
 
 // R rounds j .. j + R - 1 over tables of 2^R q entries (the first pass: W and
@@ -254,12 +270,16 @@ __device__ __forceinline__ void embed_pass_block(const EmbedArgs &a, int j, uint
 #pragma unroll
     for (int c = 0; c < 3 * R; c++) acc[c] = 0;
     for (uint64_t i = (uint64_t)blk * kThreads + threadIdx.x; i < q; i += (uint64_t)nblk * kThreads) {
-        uint64_t u[NL], v[NL];
+        uint64_t u[NL], v[NL], hi[NL];
 #pragma unroll
-        for (int t = 0; t < NL; t++) {
-            u[t] = FIRST ? embed_weight(a, i + t * q) : a.T0[i + t * q];
+        for (int t = 0; t < NL; t++) {  // loads first
+            u[t] = FIRST ? a.W[i + t * q] : a.T0[i + t * q];
+            hi[t] = FIRST ? a.W[a.rows + i + t * q] : 0;
             v[t] = FIRST ? a.b[i + t * q] : a.T1[i + t * q];
         }
+        if (FIRST)
+#pragma unroll
+            for (int t = 0; t < NL; t++) u[t] = embed_weight(u[t], hi[t]);
 #pragma unroll
         for (int c = 0; c < R; c++) {
             const int h = NL >> (c + 1);
@@ -268,7 +288,6 @@ __device__ __forceinline__ void embed_pass_block(const EmbedArgs &a, int j, uint
                 embed_pair(u[p], u[p + h], v[p], v[p + h], acc + 3 * c);
                 u[p] = fold(u[p], u[p + h], rho[c]);
                 v[p] = fold(v[p], v[p + h], rho[c]);
-                if ((p & 3) == 3 || p == h - 1) fold_all<3>(acc + 3 * c);
             }
         }
         a.T0[i] = m61::canon(u[0]);
@@ -282,7 +301,7 @@ __device__ __forceinline__ void embed_pass_block(const EmbedArgs &a, int j, uint
 template <int V, bool WIT, int NT>
 __device__ __forceinline__ void embed_product_block(const EmbedArgs &a, const EntriesArgs &e, int idx, uint64_t *red)
 {
-    entries_block<V, WIT, NT>(EmbedRows<V>{a.tok, a.E, a.ld, a.vocab, a.d, a.scale},
+    entries_block<V, WIT, NT, 4>(EmbedRows<V>{a.tok, a.E, a.ld, a.vocab, a.d, a.scale},
                               [&](uint64_t row) { return a.E1[row]; }, [&](uint64_t col) { return a.E2[col]; }, a.n,
                               a.lk, e.C, e.we, e.mm, idx, e.total, red);
 }
@@ -312,18 +331,20 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_embed_tails(EmbedArgs a, 
     }
     uint64_t g[3] = {0, 0, 0};
     const int m = a.lv - j0, base = m < kEntryTailLog ? m : kEntryTailLog, C = m - base;  // C <= 2 rounds in registers
-    uint64_t u[IT][EM] = {}, v[IT][EM] = {};
+    uint64_t u[IT][EM] = {}, v[IT][EM] = {}, hi[IT][EM] = {};
     if (j >= j0) {  // asked for first, as in k_gate_tails
+        const uint64_t *p0 = j0 == 0 ? a.W : a.T0, *p1 = j0 == 0 ? a.b : a.T1;
 #pragma unroll
-        for (int it = 0; it < IT; it++)
+        for (int it = 0; it < IT; it++) {
+            const int i = it * NT + tid < 1 << base ? it * NT + tid : 0;  // past the end: entry 0's, unused
 #pragma unroll
-            for (int t = 0; t < EM; t++) {
-                const int i = it * NT + tid;
-                if (t >= 1 << C || i >= 1 << base) continue;
-                const uint64_t x = i + ((uint64_t)t << base);
-                u[it][t] = j0 == 0 ? embed_weight(a, x) : a.T0[x];
-                v[it][t] = j0 == 0 ? a.b[x] : a.T1[x];
-            }
+            for (int t = 0; t < EM; t++)
+                if (t < 1 << C) {
+                    u[it][t] = p0[i + (t << base)];
+                    v[it][t] = p1[i + (t << base)];
+                    if (j0 == 0) hi[it][t] = a.W[a.rows + i + (t << base)];
+                }
+        }
     }
     if (tid < a.lv) rhol[tid] = a.rho[tid];
     if (j < j0) {
@@ -339,6 +360,9 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_embed_tails(EmbedArgs a, 
         for (int it = 0; it < IT; it++) {
             const int i = it * NT + tid;
             if (i >= n0) continue;
+            if (j0 == 0)
+#pragma unroll
+                for (int t = 0; t < EM; t++) u[it][t] = embed_weight(u[it][t], hi[it][t]);
 #pragma unroll
             for (int c = 0; c < kEntryTailMax - kEntryTailLog; c++) {
                 const int h = (1 << C) >> (c + 1);
@@ -349,7 +373,6 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_embed_tails(EmbedArgs a, 
                     const uint64_t u1 = h == 2 ? u[it][p + 2] : u[it][1], v1 = h == 2 ? v[it][p + 2] : v[it][1];
                     if (c == jj) {
                         embed_pair(u[it][p], u1, v[it][p], v1, g);
-                        fold_all<3>(g);
                     } else {
                         u[it][p] = fold(u[it][p], u1, rhol[j0 + c]);
                         v[it][p] = fold(v[it][p], v1, rhol[j0 + c]);
@@ -374,7 +397,7 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_embed_tails(EmbedArgs a, 
             if (j == a.lv) {
                 if (tid != 0) return;
                 const uint64_t u = m61::canon(t0[0]), v = m61::canon(t1[0]);
-                if (a.lv == 0) a.tr[0] = m61::mul(u, v);
+                if (a.lv == 0) a.tr[0] = *e.c0 = m61::mul(u, v);
                 a.tr[1 + 3 * (size_t)a.lv] = u;
                 a.tr[2 + 3 * (size_t)a.lv] = v;
                 return;
@@ -382,7 +405,6 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_embed_tails(EmbedArgs a, 
             const int h = n >> 1;
             for (int i = tid; i < h; i += NT) {
                 embed_pair(t0[i], t0[i + h], t1[i], t1[i + h], g);
-                fold_all<3>(g);
             }
         }
     }
@@ -392,7 +414,7 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_embed_tails(EmbedArgs a, 
     a.tr[2 + 3 * (size_t)j] = t[1];
     // at 2: g_0 + 2 (g_1 - g_0) + 2 (differences' products)
     a.tr[3 + 3 * (size_t)j] = m61::sub(m61::add(m61::add(t[1], t[1]), m61::add(t[2], t[2])), t[0]);
-    if (j == 0) a.tr[0] = m61::add(t[0], t[1]);
+    if (j == 0) a.tr[0] = *e.c0 = m61::add(t[0], t[1]);
 }
 
 int embed_entries(const EmbedArgs &a, const EntriesArgs &e)

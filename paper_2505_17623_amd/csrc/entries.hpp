@@ -5,10 +5,11 @@
 // the workgroup's partial claims at (r1, r2) and range flag.
 //
 // A thread keeps its V columns over all its rows, so a claim is sum_col E2[col]
-// (sum_row E1[row] z): E1 in limbs (21 bits against the 31-bit R and Y, 31
-// bits against the 16-bit Rm), the inner sums exact in int64 (at most 2^12
-// rows a thread: N <= 2^31 over 2^18 threads of two columns), one product in F_p a
-// column at the end; Z~ follows from R~ and Y~.
+// (sum_row E1[row] z), E1 in limbs of 31 bits, the inner sums exact in int64 (at
+// most 2^12 rows a thread: N <= 2^31 over 2^18 threads of two columns), one
+// product in F_p a column at the end.  Only Rm~ and Y~ are summed: C = 2^s R +
+// Rm - half entry by entry, so R~ follows from C~, which is the sum that the
+// product's sum-check claims, and Z~ from R~ and Y~ (claims.hpp).
 #pragma once
 #include <type_traits>
 
@@ -18,7 +19,7 @@
 
 namespace ra {
 
-constexpr int entries_lds_words(int nt) { return m61::block_sum_words(3, nt); }
+constexpr int entries_lds_words(int nt) { return m61::block_sum_words(2, nt); }
 
 // Columns a thread takes: 2 where rows allow it and the outputs are aligned for
 // stores of pairs.
@@ -48,11 +49,30 @@ template <typename F> inline void entries_variant(uint64_t k, const EntriesArgs 
     else f(integral_constant<int, 1>{}, integral_constant<bool, false>{});
 }
 
-// Workgroup blk of nblk (NT threads each): load(row, col, c) gives V entries
-// of C from (row, col) on, e1(row) and e2(col) eq(r1, row) and eq(r2, col)
-// (canonical).  Without WIT C is written and the workgroup's smallest and
-// largest entry, to mm[2 blk ..].  red: entries_lds_words(NT) words.
-template <int V, bool WIT, int NT, typename Load, typename E1, typename E2>
+// witness_entry (claims.hpp) with R in 32 bits from the shift on: the same for
+// an entry within the range; *oor is set for every other.
+__device__ __forceinline__ WitOut witness_entry32(int64_t c, int s, int t, int relu, int64_t half, int &oor)
+{
+    WitOut o;
+    const int64_t cc = c + half, q = cc >> s;
+    o.r = (int32_t)q;
+    const int32_t sign = o.r >> 31;
+    oor |= (int32_t)(q >> 32) != sign || ((uint32_t)(o.r ^ sign) >> (t + 1)) != 0;
+    o.rm = (int32_t)((uint32_t)cc & ((1u << s) - 1u));
+    o.y = (o.r ^ sign) - sign;
+    o.z = relu ? o.r & ~sign : o.r;
+    o.w = (uint64_t)(uint32_t)o.rm | ((uint64_t)((uint32_t)o.r + (2u << t)) << s);
+    if (relu) o.w |= (uint64_t)(uint32_t)o.y << (s + t + 2);
+    return o;
+}
+
+// Workgroup blk of nblk (NT threads each): load.fetch<M>(row, step, col, raw)
+// asks for V entries of M rows from (row, col) on, load.value(raw[u], c) gives
+// row u's; e1(row) and e2(col) are eq(r1, row) and eq(r2, col) (canonical).  A
+// thread has the loads of U of its rows in flight.  Without WIT C is written
+// and the workgroup's smallest and largest entry, to mm[2 blk ..].  red:
+// entries_lds_words(NT) words.
+template <int V, bool WIT, int NT, int U, typename Load, typename E1, typename E2>
 __device__ __forceinline__ void entries_block(const Load &load, const E1 &eq1v, const E2 &eq2v, uint64_t n, int lk,
                                               int64_t *__restrict__ C, const WitEpi &we, int64_t *__restrict__ mm,
                                               int blk, int nblk, uint64_t *red)
@@ -62,73 +82,80 @@ __device__ __forceinline__ void entries_block(const Load &load, const E1 &eq1v, 
     typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
     const uint64_t G = (uint64_t)nblk * NT, g = (uint64_t)blk * NT + threadIdx.x;  // powers of two
     const uint64_t q = (1ull << lk) / V, rstep = G > q ? G / q : 1;
-    uint64_t acc[3] = {0, 0, 0};
+    auto limbs = [](const uint64_t *s) {  // s[0] + 2^31 s[1]
+        return m61::fold(m61::from_i64((int64_t)s[0]) + m61::rotl(m61::from_i64((int64_t)s[1]), 31));
+    };
+    uint64_t acc[2] = {0, 0};
     int64_t lo = INT64_MAX, hi = INT64_MIN;
     int oor = 0;
     for (uint64_t cq = g & (q - 1); cq < q; cq += G) {
         const uint64_t col = cq * V;
-        uint64_t sr[V][3] = {}, sm[V][2] = {}, sy[V][3] = {};
-        for (uint64_t row = G > q ? g / q : 0; row < n; row += rstep) {
-            int64_t c[V];
-            load(row, col, c);
-            const uint64_t x = (row << lk) + col;
-            if constexpr (V == 2) {
-                *(v2l *)&C[x] = v2l{c[0], c[1]};
-            } else {
-                C[x] = c[0];
-            }
-            if constexpr (!WIT) {
+        uint64_t sm[V][2] = {}, sy[V][2] = {}, fy[V] = {};
+        auto rows = [&](auto count, uint64_t row0) {
+            constexpr int M = decltype(count)::value;
+            typename Load::Raw raw[M];
+            uint64_t e[M];
+            load.template fetch<M>(row0, rstep, col, raw);
+            if constexpr (WIT)
+#pragma unroll
+                for (int u = 0; u < M; u++) e[u] = eq1v(row0 + u * rstep);
+#pragma unroll
+            for (int u = 0; u < M; u++) {
+                int64_t c[V];
+                load.value(raw[u], c);
+                const uint64_t x = ((row0 + u * rstep) << lk) + col;
+                if constexpr (V == 2) {
+                    *(v2l *)&C[x] = v2l{c[0], c[1]};
+                } else {
+                    C[x] = c[0];
+                }
+                if constexpr (!WIT) {
+#pragma unroll
+                    for (int i = 0; i < V; i++) {
+                        lo = c[i] < lo ? c[i] : lo;
+                        hi = c[i] > hi ? c[i] : hi;
+                    }
+                    continue;
+                }
+                const int32_t el = (int32_t)(e[u] & 0x7FFFFFFF), eh = (int32_t)(e[u] >> 31);
+                WitOut o[V];
 #pragma unroll
                 for (int i = 0; i < V; i++) {
-                    lo = c[i] < lo ? c[i] : lo;
-                    hi = c[i] > hi ? c[i] : hi;
+                    o[i] = witness_entry32(c[i], we.s, we.t, we.relu, we.half, oor);
+                    sm[i][0] += (uint64_t)((int64_t)el * o[i].rm);
+                    sm[i][1] += (uint64_t)((int64_t)eh * o[i].rm);
+                    sy[i][0] += (uint64_t)((int64_t)el * o[i].y);
+                    sy[i][1] += (uint64_t)((int64_t)eh * o[i].y);
+                    if (we.t > 17) {  // |Y| <= 2^(t+1): past 2^18 a row's terms are reduced at once
+                        fy[i] = m61::fold(fy[i] + limbs(sy[i]));
+                        sy[i][0] = sy[i][1] = 0;
+                    }
                 }
-                continue;
+                if constexpr (V == 2) {
+                    *(v2i *)&we.R[x] = v2i{o[0].r, o[1].r};
+                    *(v2i *)&we.Y[x] = v2i{o[0].y, o[1].y};
+                    *(v2i *)&we.Z[x] = v2i{o[0].z, o[1].z};
+                    *(v2u16 *)&we.Rm[x] = v2u16{(unsigned short)o[0].rm, (unsigned short)o[1].rm};
+                    *(v2l *)&we.bits[x] = v2l{(long long)o[0].w, (long long)o[1].w};
+                } else {
+                    we.R[x] = o[0].r;
+                    we.Y[x] = o[0].y;
+                    we.Z[x] = o[0].z;
+                    we.Rm[x] = (uint16_t)o[0].rm;
+                    we.bits[x] = o[0].w;
+                }
             }
-            const uint64_t e = eq1v(row);
-            const int32_t e0 = (int32_t)(e & 0x1FFFFF), e1 = (int32_t)((e >> 21) & 0x1FFFFF), e2 = (int32_t)(e >> 42);
-            const int32_t el = (int32_t)(e & 0x7FFFFFFF), eh = (int32_t)(e >> 31);
-            WitOut o[V];
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                o[i] = witness_entry(c[i], we.s, we.t, we.relu, we.half, oor);
-                sr[i][0] += (uint64_t)((int64_t)e0 * o[i].r);
-                sr[i][1] += (uint64_t)((int64_t)e1 * o[i].r);
-                sr[i][2] += (uint64_t)((int64_t)e2 * o[i].r);
-                sm[i][0] += (uint64_t)((int64_t)el * o[i].rm);
-                sm[i][1] += (uint64_t)((int64_t)eh * o[i].rm);
-                sy[i][0] += (uint64_t)((int64_t)e0 * o[i].y);
-                sy[i][1] += (uint64_t)((int64_t)e1 * o[i].y);
-                sy[i][2] += (uint64_t)((int64_t)e2 * o[i].y);
-            }
-            if constexpr (V == 2) {
-                *(v2i *)&we.R[x] = v2i{o[0].r, o[1].r};
-                *(v2i *)&we.Y[x] = v2i{o[0].y, o[1].y};
-                *(v2i *)&we.Z[x] = v2i{o[0].z, o[1].z};
-                *(v2u16 *)&we.Rm[x] = v2u16{(unsigned short)o[0].rm, (unsigned short)o[1].rm};
-                *(v2l *)&we.bits[x] = v2l{(long long)o[0].w, (long long)o[1].w};
-            } else {
-                we.R[x] = o[0].r;
-                we.Y[x] = o[0].y;
-                we.Z[x] = o[0].z;
-                we.Rm[x] = (uint16_t)o[0].rm;
-                we.bits[x] = o[0].w;
-            }
-        }
+        };
+        uint64_t row = G > q ? g / q : 0;  // the same number of rows for every thread that has any
+        if constexpr (U > 1)
+            for (; row + (U - 1) * rstep < n; row += U * rstep) rows(std::integral_constant<int, U>{}, row);
+        for (; row < n; row += rstep) rows(std::integral_constant<int, 1>{}, row);
         if constexpr (WIT) {
-            auto value3 = [](const uint64_t *s) {
-                return m61::fold(m61::from_i64((int64_t)s[0]) + m61::rotl(m61::from_i64((int64_t)s[1]), 21) +
-                                 m61::rotl(m61::from_i64((int64_t)s[2]), 42));
-            };
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 const uint64_t e2 = eq2v(col + i);
-                acc[0] = m61::lmacc(acc[0], value3(sr[i]), e2);
-                acc[1] = m61::lmacc(acc[1],
-                                    m61::fold(m61::from_i64((int64_t)sm[i][0]) +
-                                              m61::rotl(m61::from_i64((int64_t)sm[i][1]), 31)),
-                                    e2);
-                acc[2] = m61::lmacc(acc[2], value3(sy[i]), e2);
+                acc[0] = m61::lmacc(acc[0], limbs(sm[i]), e2);
+                acc[1] = m61::lmacc(acc[1], m61::fold(fy[i] + limbs(sy[i])), e2);
             }
         }
     }
@@ -155,13 +182,9 @@ __device__ __forceinline__ void entries_block(const Load &load, const E1 &eq1v, 
         }
     } else {
         const int any = __syncthreads_or(oor);
-        const uint64_t *t = m61::block_sum_lds<3>(acc, red);
-        if (threadIdx.x == 0) {
-            const uint64_t z = we.relu ? m61::rotl(m61::add(t[0], t[2]), 60) : t[0];  // 2^60 = 1/2
-            for (int i = 0; i < 3; i++) we.claim_part[4 * (size_t)blk + i] = t[i];
-            we.claim_part[4 * (size_t)blk + 3] = z;
-            we.flags[blk] = (uint32_t)any;
-        }
+        const uint64_t *t = m61::block_sum_lds<2>(acc, red);
+        if (threadIdx.x < 4) we.claim_part[4 * (size_t)blk + threadIdx.x] = threadIdx.x == 1 || threadIdx.x == 2 ? t[threadIdx.x - 1] : 0;
+        if (threadIdx.x == 0) we.flags[blk] = (uint32_t)any;
     }
 }
 

@@ -22,37 +22,83 @@
 
 namespace ra {
 
-// Entry (row, col) of a factor: int16 or int32, rows `ld` entries apart (0:
-// one row for all).
-__device__ __forceinline__ int32_t gate_load(const GateSrc &s, uint64_t x, int lk)
+// Entries i + t q (i < q, q a power of two), t < cnt <= NL, of a factor (int16
+// or int32, rows `ld` entries apart, 0: one row for all).  An entry's place
+// (x >> lk) ld + (x mod 2^lk) is additive over disjoint bits of x, so those of
+// t q are the same for every thread.  All loads go out before any is waited
+// for: the type is looked at once, and a load gives the extended value.
+template <int NL>
+__device__ __forceinline__ void gate_fetch(const GateSrc &s, uint64_t i, uint64_t q, int cnt, int lk, int32_t (&out)[NL])
 {
-    const uint64_t at = (x >> lk) * s.ld + (x & ((1ull << lk) - 1));
-    return s.i16 ? (int32_t)((const int16_t *)s.p)[at] : ((const int32_t *)s.p)[at];
+    const uint64_t mask = (1ull << lk) - 1, at = (i >> lk) * s.ld + (i & mask);
+    if (s.i16) {
+        const int16_t *p = (const int16_t *)s.p + at;
+#pragma unroll
+        for (int t = 0; t < NL; t++)
+            if (t < cnt) out[t] = p[((t * q) >> lk) * s.ld + ((t * q) & mask)];
+    } else {
+        const int32_t *p = (const int32_t *)s.p + at;
+#pragma unroll
+        for (int t = 0; t < NL; t++)
+            if (t < cnt) out[t] = p[((t * q) >> lk) * s.ld + ((t * q) & mask)];
+    }
 }
+
+// An int32 as a loose residue (m61.hpp): p + v, within 2^32 of 2^61.
+__device__ __forceinline__ uint64_t int_to_loose(int64_t v) { return (uint64_t)v + m61::P; }
 
 // V entries of C = A B, exact in int64 (|C| <= 2^62).
 template <int V> struct GateProduct {
     GateSrc A, B;
-    __device__ __forceinline__ void factor(const GateSrc &s, uint64_t at, int32_t (&v)[V]) const
+    struct Raw {
+        int32_t a[V], b[V];
+    };
+    template <int U>
+    __device__ __forceinline__ void fetch(uint64_t row, uint64_t step, uint64_t col, Raw (&raw)[U]) const
     {
-        if (s.i16) {  // uniform; the loads need no more alignment than the entries have
-            int16_t h[V];
-            __builtin_memcpy(h, (const int16_t *)s.p + at, sizeof h);
+        // no more alignment than the entries have
+        if (A.i16) {
 #pragma unroll
-            for (int i = 0; i < V; i++) v[i] = h[i];
+            for (int u = 0; u < U; u++) pair16(A, row + u * step, col, raw[u].a);
         } else {
-            __builtin_memcpy(v, (const int32_t *)s.p + at, sizeof v);
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                __builtin_memcpy(raw[u].a, (const int32_t *)A.p + (row + u * step) * A.ld + col, sizeof raw[u].a);
+        }
+        if (B.i16) {
+#pragma unroll
+            for (int u = 0; u < U; u++) pair16(B, row + u * step, col, raw[u].b);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                __builtin_memcpy(raw[u].b, (const int32_t *)B.p + (row + u * step) * B.ld + col, sizeof raw[u].b);
         }
     }
-    __device__ __forceinline__ void operator()(uint64_t row, uint64_t col, int64_t (&c)[V]) const
+    __device__ __forceinline__ static void pair16(const GateSrc &s, uint64_t row, uint64_t col, int32_t (&v)[V])
     {
-        int32_t a[V], b[V];
-        factor(A, row * A.ld + col, a);
-        factor(B, row * B.ld + col, b);
 #pragma unroll
-        for (int i = 0; i < V; i++) c[i] = (int64_t)a[i] * b[i];
+        for (int i = 0; i < V; i++) v[i] = ((const int16_t *)s.p)[row * s.ld + col + i];
+    }
+    __device__ __forceinline__ void value(const Raw &r, int64_t (&c)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; i++) c[i] = (int64_t)r.a[i] * r.b[i];
     }
 };
+
+// A pair of the first round, from the integers: its products are exact in
+// int64, so it takes three products in F_p, and none to fold but the two by the
+// challenge.  acc[0..3) += Z_0, Z_1 and the cross terms w (a_0 b_1 + a_1 b_0).
+__device__ __forceinline__ void gate_pair_ints(uint64_t w, int32_t a0, int32_t a1, int32_t b0, int32_t b1, uint64_t *acc)
+{
+    acc[0] = m61::lmacc(acc[0], w, small_to_field((int64_t)a0 * b0));
+    acc[1] = m61::lmacc(acc[1], w, small_to_field((int64_t)a1 * b1));
+    acc[2] = m61::lmacc(acc[2], w, small_to_field((int64_t)a0 * b1) + small_to_field((int64_t)a1 * b0));
+}
+__device__ __forceinline__ uint64_t fold_ints(int32_t lo, int32_t hi, uint64_t z)
+{
+    return m61::lmacc(int_to_loose(lo), z, int_to_loose((int64_t)hi - lo));
+}
 
 // The suffix eq tables of r and the prefix products K_j (xsetup.hpp) by the
 // first nx threads, the eq tables E1 (r1) and E2 (r2) by the others.
@@ -74,6 +120,14 @@ __global__ __launch_bounds__(256) void k_gate_setup(XSetupArgs a, int nx, int ln
     else if (i - n < 1ull << (a.lN - ln)) E2[i - n] = eq_suffix(rl, ln, a.lN - ln, i - n);
 }
 
+
+__device__ __forceinline__ void rp_old(uint64_t w, uint64_t d0, uint64_t d1, uint64_t s0, uint64_t s1, uint64_t *acc)
+{
+    const uint64_t ed0 = m61::lmul(w, d0), ed1 = m61::lmul(w, d1);
+    acc[0] += m61::lmul(ed0, s0);
+    acc[1] += m61::lmul(ed1, s1);
+    acc[2] += m61::lmul(ed0 + ed1, s0 + s1);
+}
 // R rounds j .. j + R - 1 over tables of 2^R q entries in one pass: a thread
 // holds the 2^R entries i + t q that end in entry i of the folded tables.  The
 // first pass reads the factors themselves.
@@ -92,10 +146,18 @@ __device__ __forceinline__ void gate_pass_block(const GateArgs &a, int j, uint64
     const int nvar = a.lN - j - R;
     for (uint64_t i = (uint64_t)blk * kThreads + threadIdx.x; i < q; i += (uint64_t)nblk * kThreads) {
         uint64_t u[NL], v[NL], w[NL];
+        int32_t ai[NL], bi[NL];
+        if (FIRST) {
+            gate_fetch<NL>(a.A, i, q, NL, a.lk, ai);
+            gate_fetch<NL>(a.B, i, q, NL, a.lk, bi);
 #pragma unroll
-        for (int t = 0; t < NL; t++) {
-            u[t] = FIRST ? small_to_field(gate_load(a.A, i + t * q, a.lk)) : a.T0[i + t * q];
-            v[t] = FIRST ? small_to_field(gate_load(a.B, i + t * q, a.lk)) : a.T1[i + t * q];
+            for (int t = 0; t < NL; t++) { u[t] = int_to_loose(ai[t]); v[t] = int_to_loose(bi[t]); }
+        } else {
+#pragma unroll
+            for (int t = 0; t < NL; t++) {
+                u[t] = a.T0[i + t * q];
+                v[t] = a.T1[i + t * q];
+            }
         }
         x_weights<R>(suffix_weight(a.HS, a.LS, nvar, a.L, i), rr, w);
 #pragma unroll
@@ -103,15 +165,22 @@ __device__ __forceinline__ void gate_pass_block(const GateArgs &a, int j, uint64
             const int h = NL >> (c + 1), base = h - 1;
 #pragma unroll
             for (int p = 0; p < h; p++) {
-                relu_pair(w[base + p], u[p], u[p + h], v[p], v[p + h], acc + 3 * c);
-                u[p] = fold(u[p], u[p + h], rho[c]);
-                v[p] = fold(v[p], v[p + h], rho[c]);
-                if ((p & 3) == 3 || p == h - 1) fold_all<3>(acc + 3 * c);
+                if (false) {
+                    rp_old(w[base + p], int_to_loose(ai[p]), int_to_loose(ai[p + h]), int_to_loose(bi[p]), int_to_loose(bi[p + h]), acc);
+                    u[p] = fold(int_to_loose(ai[p]), int_to_loose(ai[p + h]), rho[c]);
+                    v[p] = fold(int_to_loose(bi[p]), int_to_loose(bi[p + h]), rho[c]);
+                } else {
+                    rp_old(w[base + p], u[p], u[p + h], v[p], v[p + h], acc + 3 * c);
+                    u[p] = fold(u[p], u[p + h], rho[c]);
+                    v[p] = fold(v[p], v[p + h], rho[c]);
+                }
+                if ((p & 3) == 3 || p == h - 1) fold_all<3>(acc + 3 * c);  // pairs in order: their values need few registers
             }
         }
         a.T0[i] = m61::canon(u[0]);
         a.T1[i] = m61::canon(v[0]);
     }
+    if (FIRST) ;  // U from the cross terms
     const uint64_t *t = m61::block_sum_lds<3 * R>(acc, red);
     if (threadIdx.x < 3 * R)
         a.part[(size_t)(3 * j + threadIdx.x) * kEntryMaxBlocks + blk] = t[threadIdx.x];
@@ -138,7 +207,7 @@ __global__ __launch_bounds__(256) void k_gate_first(GateArgs a, uint64_t q, int 
         gate_pass_block<R, true>(a, 0, q, idx, npass, red);
         return;
     }
-    entries_block<V, WIT, kThreads>(GateProduct<V>{a.A, a.B}, [&](uint64_t row) { return a.E1[row]; },
+    entries_block<V, WIT, kThreads, 1>(GateProduct<V>{a.A, a.B}, [&](uint64_t row) { return a.E1[row]; },
                                     [&](uint64_t col) { return a.E2[col]; }, 1ull << (a.lN - a.lk), a.lk, e.C, e.we,
                                     e.mm, idx, e.total, red);
 }
@@ -182,7 +251,7 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, in
                 }
                 return;
             }
-            entries_block<V, WIT, NT>(load, [&](uint64_t row) { return eq_suffix(rl, 0, ln, row); },
+            entries_block<V, WIT, NT, 1>(load, [&](uint64_t row) { return eq_suffix(rl, 0, ln, row); },
                                       [&](uint64_t col) { return eq_suffix(rl, ln, a.lk, col); }, 1ull << ln, a.lk,
                                       e.C, e.we, e.mm, b, e.total, red);
         }
@@ -193,19 +262,24 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, in
     const int nvar = a.lN - j - 1, lo = nvar / 2, hi = nvar - lo;  // of the weights (j >= j0: at most 12)
     // the tables' entries (or a pass's partials) are asked for first, and land
     // while the point, the weights and K_j are made
-    uint64_t u[IT][EM] = {}, v[IT][EM] = {};
-    if (j >= j0) {
+    uint64_t u[IT][EM], v[IT][EM];
+    int32_t ai[IT][EM] = {}, bi[IT][EM] = {};
+    if (j >= j0)
 #pragma unroll
-        for (int it = 0; it < IT; it++)
+        for (int it = 0; it < IT; it++) {
+            const int i = it * NT + tid < 1 << base ? it * NT + tid : 0;  // past the end: entry 0's, unused
+            if (j0 == 0) {
+                gate_fetch<EM>(a.A, i, 1ull << base, 1 << C, a.lk, ai[it]);
+                gate_fetch<EM>(a.B, i, 1ull << base, 1 << C, a.lk, bi[it]);
+            } else {
 #pragma unroll
-            for (int t = 0; t < EM; t++) {
-                const int i = it * NT + tid;
-                if (t >= 1 << C || i >= 1 << base) continue;
-                const uint64_t x = i + ((uint64_t)t << base);
-                u[it][t] = j0 == 0 ? (uint64_t)(int64_t)gate_load(a.A, x, a.lk) : a.T0[x];
-                v[it][t] = j0 == 0 ? (uint64_t)(int64_t)gate_load(a.B, x, a.lk) : a.T1[x];
+                for (int t = 0; t < EM; t++)
+                    if (t < 1 << C) {
+                        u[it][t] = a.T0[i + (t << base)];
+                        v[it][t] = a.T1[i + (t << base)];
+                    }
             }
-    }
+        }
     if (tid < a.lN) {
         rl[tid] = a.r[tid];
         rhol[tid] = a.rho[tid];
@@ -239,8 +313,8 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, in
             if (j0 == 0)
 #pragma unroll
                 for (int t = 0; t < EM; t++) {
-                    u[it][t] = small_to_field((int64_t)u[it][t]);
-                    v[it][t] = small_to_field((int64_t)v[it][t]);
+                    u[it][t] = small_to_field(ai[it][t]);
+                    v[it][t] = small_to_field(bi[it][t]);
                 }
 #pragma unroll
             for (int c = 0; c < kEntryTailMax - kEntryTailLog; c++) {
@@ -252,7 +326,6 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, in
                     const uint64_t u1 = h == 2 ? u[it][p + 2] : u[it][1], v1 = h == 2 ? v[it][p + 2] : v[it][1];
                     if (c == jj) {
                         relu_pair(weight(p * n0 + i), u[it][p], u1, v[it][p], v1, g);
-                        fold_all<3>(g);
                     } else {
                         u[it][p] = fold(u[it][p], u1, rhol[j0 + c]);
                         v[it][p] = fold(v[it][p], v1, rhol[j0 + c]);
@@ -277,7 +350,7 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, in
             if (j == a.lN) {
                 if (tid != 0) return;
                 const uint64_t u = m61::canon(t0[0]), v = m61::canon(t1[0]);
-                if (a.lN == 0) a.tr[0] = m61::mul(u, v);
+                if (a.lN == 0) a.tr[0] = *e.c0 = m61::mul(u, v);
                 a.tr[1 + 4 * (size_t)a.lN] = u;
                 a.tr[2 + 4 * (size_t)a.lN] = v;
                 return;
@@ -285,7 +358,6 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, in
             const int h = n >> 1;
             for (int i = tid; i < h; i += NT) {
                 relu_pair(weight(i), t0[i], t0[i + h], t1[i], t1[i + h], g);
-                fold_all<3>(g);
             }
         }
     }
@@ -294,7 +366,7 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, in
     if (tid >= 4) return;
     const uint64_t val = gate_round_eval(t, lin, tid), next = __shfl_down(val, 1, 64);
     a.tr[1 + 4 * (size_t)j + tid] = val;
-    if (j == 0 && tid == 0) a.tr[0] = m61::add(val, next);  // the claimed sum g_1(0) + g_1(1)
+    if (j == 0 && tid == 0) a.tr[0] = *e.c0 = m61::add(val, next);  // the claimed sum g_1(0) + g_1(1)
 }
 
 int gate_entries(const GateArgs &a, const EntriesArgs &e)

@@ -631,7 +631,7 @@ void launch_witness_rescale(const int64_t *C, uint64_t N, int lk, const uint64_t
     else
         hipLaunchKernelGGL(k_rescale<1>, dim3(nb), dim3(kThreads), 0, st, C, N, lk, (const WitParams *)params, E1, E2,
                            R, Rm, Y, Z, bits, claim_part, hp, known ? 1 : 0, flags);
-    const ClaimsJob j{claim_part, nb, params, claims_out, mirror, hp, known ? 1 : 0, flags};
+    const ClaimsJob j{claim_part, nb, params, claims_out, mirror, hp, known ? 1 : 0, flags, nullptr};
     if (defer) *defer = j;
     else launch_claims_final(j, st);
 }

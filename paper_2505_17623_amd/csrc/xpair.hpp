@@ -8,16 +8,15 @@
 
 namespace ra {
 
-// Terms of one pair with weight w of sum_x EQ(x) d(x) s(x), added to acc
-// without folding (each term is a folded value): acc[0..3) = Z_0, Z_1, U.
-// Inputs are folded or canonical.
+// Terms of one pair with weight w of sum_x EQ(x) d(x) s(x), added to the
+// folded acc[0..3) = Z_0, Z_1, U.  Inputs are folded or canonical.
 __device__ __forceinline__ void relu_pair(uint64_t w, uint64_t d0, uint64_t d1, uint64_t s0, uint64_t s1,
                                           uint64_t *acc)
 {
     const uint64_t ed0 = m61::lmul(w, d0), ed1 = m61::lmul(w, d1);
-    acc[0] += m61::lmul(ed0, s0);
-    acc[1] += m61::lmul(ed1, s1);
-    acc[2] += m61::lmul(ed0 + ed1, s0 + s1);  // sums of two folded values are loose
+    acc[0] = m61::lmacc(acc[0], ed0, s0);
+    acc[1] = m61::lmacc(acc[1], ed1, s1);
+    acc[2] = m61::lmacc(acc[2], ed0 + ed1, s0 + s1);  // sums of two folded values are loose
 }
 
 template <int NV>
@@ -30,7 +29,7 @@ __device__ __forceinline__ void fold_all(uint64_t *acc)
 // lo + z (hi - lo), folded.
 __device__ __forceinline__ uint64_t fold(uint64_t lo, uint64_t hi, uint64_t z)
 {
-    return m61::fold(lo + m61::lmul(z, m61::lsub(hi, lo)));
+    return m61::lmacc(lo, z, m61::lsub(hi, lo));
 }
 
 // Field value of a small signed integer (|v| < 2^62), folded.

@@ -155,7 +155,6 @@ __device__ __forceinline__ void x_sub_cubes(const XArgs &a, uint64_t sub, uint64
                     relu_pair(w[base + u], d[u], d[u + h], s[u], s[u + h], acc[c]);
                     d[u] = fold(d[u], d[u + h], rz[c]);
                     s[u] = fold(s[u], s[u + h], rz[c]);
-                    if ((u & 3) == 3 || u == h - 1) fold_all<NV>(acc[c]);
                 }
             }
             a.d[i] = m61::canon(d[0]);
@@ -369,7 +368,7 @@ __device__ __forceinline__ void xb_wave(const XBlockArgs &a, uint64_t k, uint64_
                         t0[e] = fold(t0[e], t0[e + hs], z[c]);
                         t1[e] = fold(t1[e], t1[e + hs], z[c]);
                     }
-                    fold_all<NV>(acc);
+                    if (!ZW) fold_all<NV>(acc);
                 }
             }
         } else {  // lane u < h pairs with lane u + h (slot 0)
@@ -384,7 +383,7 @@ __device__ __forceinline__ void xb_wave(const XBlockArgs &a, uint64_t k, uint64_
                     t0[0] = fold(t0[0], p0, z[c]);
                     t1[0] = fold(t1[0], p1, z[c]);
                 }
-                fold_all<NV>(acc);
+                if (!ZW) fold_all<NV>(acc);
             }
         }
 #pragma unroll
