@@ -328,7 +328,7 @@ ra_status finish(ra_ctx *c, size_t off, std::function<ra_status(const uint64_t *
 }
 
 // A refused embedding found at a wait of its own layer gives its challenges
-// back and leaves the context between layers.
+// back and leaves the context between layers, its announced witness dropped.
 void take_back(ra_ctx *c)
 {
     if (!c->refused) return;
@@ -336,6 +336,7 @@ void take_back(ra_ctx *c)
     c->refused = 0;
     c->phase = 0;
     c->mm_of = nullptr;
+    c->plan.valid = c->plan.fused = false;
 }
 
 // Plane count of the bit table for given s, t, relu (the rule of the witness
@@ -673,6 +674,7 @@ ra_status ra_ctx_set_deferred(ra_ctx *c, int on)
     if (!on && c->deferred) {
         const ra_status r = drain(c);
         if (r != RA_OK && c->deferred_err == RA_OK) c->deferred_err = r;
+        c->refused = 0;
     }
     c->deferred = on != 0;
     return RA_OK;
@@ -1754,6 +1756,7 @@ void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need, const Entries
     c->phase = 1;
     c->link_ok = false;
     c->is_matrix = false;
+    c->refused = 0;
     c->plan.fused = e.wit != 0;
     c->plan.ntiles = (uint32_t)e.total;
     c->mm_of = e.wit ? nullptr : e.C;
@@ -1771,11 +1774,12 @@ extern "C" ra_status ra_gate_workspace_size(uint32_t n, uint32_t k, size_t *byte
     return RA_OK;
 }
 
-extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype, uint64_t lda, const void *d_B,
-                                   ra_dtype b_dtype, uint64_t ldb, uint32_t n, uint32_t k, int64_t *d_C, void *d_ws,
-                                   size_t ws_bytes, ra_gate_proof *out)
+namespace {
+ra_status gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype, uint64_t lda, const void *d_B,
+                     ra_dtype b_dtype, uint64_t ldb, uint32_t n, uint32_t k, int64_t *d_C, void *d_ws, size_t ws_bytes,
+                     ra_gate_proof *out)
 {
-    if (!c || !d_A || !d_B || !d_C || !out) return RA_E_INVAL;
+    if (!d_A || !d_B || !d_C || !out) return RA_E_INVAL;
     if (!is_pow2(n) || !is_pow2(k)) return RA_E_INVAL;
     if ((a_dtype != RA_I16 && a_dtype != RA_I32) || (b_dtype != RA_I16 && b_dtype != RA_I32)) return RA_E_INVAL;
     if ((lda && lda < k) || (ldb && ldb < k)) return RA_E_INVAL;
@@ -1829,6 +1833,20 @@ extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype,
     });
 }
 
+}  // namespace
+
+// A call that is refused spends an announced witness too: its buffers may not
+// outlive the call.
+extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype, uint64_t lda, const void *d_B,
+                                   ra_dtype b_dtype, uint64_t ldb, uint32_t n, uint32_t k, int64_t *d_C, void *d_ws,
+                                   size_t ws_bytes, ra_gate_proof *out)
+{
+    if (!c) return RA_E_INVAL;
+    const ra_status st = gate_prove(c, d_A, a_dtype, lda, d_B, b_dtype, ldb, n, k, d_C, d_ws, ws_bytes, out);
+    if (st != RA_OK && c->phase == 0) c->plan.valid = false;
+    return st;
+}
+
 extern "C" ra_status ra_embed_workspace_size(uint32_t n, uint32_t vocab, uint32_t d, size_t *bytes)
 {
     if (!bytes || !is_pow2(n) || !vocab || !d) return RA_E_INVAL;
@@ -1839,11 +1857,11 @@ extern "C" ra_status ra_embed_workspace_size(uint32_t n, uint32_t vocab, uint32_
     return RA_OK;
 }
 
-extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde,
-                                    uint32_t vocab, uint32_t d, int32_t scale, int64_t *d_C, void *d_ws,
-                                    size_t ws_bytes, ra_matmul_proof *out)
+namespace {
+ra_status embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde, uint32_t vocab,
+                      uint32_t d, int32_t scale, int64_t *d_C, void *d_ws, size_t ws_bytes, ra_matmul_proof *out)
 {
-    if (!c || !d_tokens || !d_E || !d_C || !out) return RA_E_INVAL;
+    if (!d_tokens || !d_E || !d_C || !out) return RA_E_INVAL;
     if (!is_pow2(n) || !vocab || !d || lde < d) return RA_E_INVAL;
     if (vocab > kEmbedMaxVocab || d > kEmbedMaxWidth) return RA_E_NOT_IMPLEMENTED;
     const int ln = log2u(n), lk = log2u(d), lv = log2u(vocab);
@@ -1907,6 +1925,18 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
     });
     take_back(c);
     return r;
+}
+
+}  // namespace
+
+extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde,
+                                    uint32_t vocab, uint32_t d, int32_t scale, int64_t *d_C, void *d_ws,
+                                    size_t ws_bytes, ra_matmul_proof *out)
+{
+    if (!c) return RA_E_INVAL;
+    const ra_status st = embed_prove(c, d_tokens, n, d_E, lde, vocab, d, scale, d_C, d_ws, ws_bytes, out);
+    if (st != RA_OK && c->phase == 0) c->plan.valid = false;
+    return st;
 }
 
 // ---------------------------------------------------------------------------

@@ -502,7 +502,7 @@ struct EntriesArgs {
 // where that takes no further pass (the last rounds' time grows with them).
 constexpr int kEntryPass = 3, kEntryTailLog = 11, kEntryTailMax = 13;
 constexpr int kEntryTailThreads = 512;
-constexpr int kEntryMaxBlocks = 512;   // blocks of a pass (partials per round)
+constexpr int kEntryMaxBlocks = 1024;  // blocks of a pass (partials per round; at most kMaxBlocks)
 __host__ __device__ inline int entry_passes(int v)
 {
     return v > kEntryTailMax ? (v - kEntryTailMax + kEntryPass - 1) / kEntryPass : 0;

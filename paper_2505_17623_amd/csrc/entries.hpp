@@ -66,6 +66,41 @@ __device__ __forceinline__ WitOut witness_entry32(int64_t c, int s, int t, int r
     return o;
 }
 
+// The workgroup's witness partial: its sums of Rm~ and Y~ and its range flag.
+template <int NT>
+__device__ __forceinline__ void entries_claims(const uint64_t (&acc)[2], int oor, const WitEpi &we, int blk, uint64_t *red)
+{
+    const int any = __syncthreads_or(oor);
+    const uint64_t *t = m61::block_sum_lds<2>(acc, red);
+    if (threadIdx.x < 4)
+        we.claim_part[4 * (size_t)blk + threadIdx.x] = threadIdx.x == 1 || threadIdx.x == 2 ? t[threadIdx.x - 1] : 0;
+    if (threadIdx.x == 0) we.flags[blk] = (uint32_t)any;
+}
+// The workgroup's smallest and largest entry, to mm[2 blk ..].
+template <int NT>
+__device__ __forceinline__ void entries_extremes(int64_t lo, int64_t hi, int64_t *mm, int blk, uint64_t *red)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        const int64_t a = __shfl_xor(lo, off, 64), b = __shfl_xor(hi, off, 64);
+        lo = a < lo ? a : lo;
+        hi = b > hi ? b : hi;
+    }
+    int64_t *w = (int64_t *)red;
+    if ((threadIdx.x & 63) == 0) {
+        w[2 * (threadIdx.x >> 6)] = lo;
+        w[2 * (threadIdx.x >> 6) + 1] = hi;
+    }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int v = 1; v < NT / 64; v++) {
+        lo = w[2 * v] < lo ? w[2 * v] : lo;
+        hi = w[2 * v + 1] > hi ? w[2 * v + 1] : hi;
+    }
+    mm[2 * blk] = lo;
+    mm[2 * blk + 1] = hi;
+}
+
 // Workgroup blk of nblk (NT threads each): load.fetch<M>(row, step, col, raw)
 // asks for V entries of M rows from (row, col) on, load.value(raw[u], c) gives
 // row u's; e1(row) and e2(col) are eq(r1, row) and eq(r2, col) (canonical).  A
@@ -159,33 +194,8 @@ __device__ __forceinline__ void entries_block(const Load &load, const E1 &eq1v, 
             }
         }
     }
-    if constexpr (!WIT) {
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            const int64_t a = __shfl_xor(lo, off, 64), b = __shfl_xor(hi, off, 64);
-            lo = a < lo ? a : lo;
-            hi = b > hi ? b : hi;
-        }
-        int64_t *w = (int64_t *)red;
-        if ((threadIdx.x & 63) == 0) {
-            w[2 * (threadIdx.x >> 6)] = lo;
-            w[2 * (threadIdx.x >> 6) + 1] = hi;
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int v = 1; v < NT / 64; v++) {
-                lo = w[2 * v] < lo ? w[2 * v] : lo;
-                hi = w[2 * v + 1] > hi ? w[2 * v + 1] : hi;
-            }
-            mm[2 * blk] = lo;
-            mm[2 * blk + 1] = hi;
-        }
-    } else {
-        const int any = __syncthreads_or(oor);
-        const uint64_t *t = m61::block_sum_lds<2>(acc, red);
-        if (threadIdx.x < 4) we.claim_part[4 * (size_t)blk + threadIdx.x] = threadIdx.x == 1 || threadIdx.x == 2 ? t[threadIdx.x - 1] : 0;
-        if (threadIdx.x == 0) we.flags[blk] = (uint32_t)any;
-    }
+    if constexpr (WIT) entries_claims<NT>(acc, oor, we, blk, red);
+    else entries_extremes<NT>(lo, hi, mm, blk, red);
 }
 
 }  // namespace ra

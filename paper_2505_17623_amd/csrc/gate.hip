@@ -86,20 +86,6 @@ template <int V> struct GateProduct {
     }
 };
 
-// A pair of the first round, from the integers: its products are exact in
-// int64, so it takes three products in F_p, and none to fold but the two by the
-// challenge.  acc[0..3) += Z_0, Z_1 and the cross terms w (a_0 b_1 + a_1 b_0).
-__device__ __forceinline__ void gate_pair_ints(uint64_t w, int32_t a0, int32_t a1, int32_t b0, int32_t b1, uint64_t *acc)
-{
-    acc[0] = m61::lmacc(acc[0], w, small_to_field((int64_t)a0 * b0));
-    acc[1] = m61::lmacc(acc[1], w, small_to_field((int64_t)a1 * b1));
-    acc[2] = m61::lmacc(acc[2], w, small_to_field((int64_t)a0 * b1) + small_to_field((int64_t)a1 * b0));
-}
-__device__ __forceinline__ uint64_t fold_ints(int32_t lo, int32_t hi, uint64_t z)
-{
-    return m61::lmacc(int_to_loose(lo), z, int_to_loose((int64_t)hi - lo));
-}
-
 // The suffix eq tables of r and the prefix products K_j (xsetup.hpp) by the
 // first nx threads, the eq tables E1 (r1) and E2 (r2) by the others.
 __global__ __launch_bounds__(256) void k_gate_setup(XSetupArgs a, int nx, int ln, uint64_t *E1, uint64_t *E2)
@@ -128,88 +114,145 @@ __device__ __forceinline__ void rp_old(uint64_t w, uint64_t d0, uint64_t d1, uin
     acc[1] += m61::lmul(ed1, s1);
     acc[2] += m61::lmul(ed0 + ed1, s0 + s1);
 }
+// C rounds of one sub-cube held in registers (u, v folded or loose), weights w
+// (x_weights): round c's sums added to acc[3 c ..], folded every fourth pair.
+template <int R>
+__device__ __forceinline__ void gate_rounds(uint64_t (&u)[1 << R], uint64_t (&v)[1 << R], const uint64_t (&w)[1 << R],
+                                            const uint64_t (&rho)[R], uint64_t (&acc)[3 * R])
+{
+#pragma unroll
+    for (int c = 0; c < R; c++) {
+        const int h = (1 << R) >> (c + 1), base = h - 1;
+#pragma unroll
+        for (int p = 0; p < h; p++) {
+            // the terms summed before a fold, not folded into the sum one by
+            // one: that order takes 50 more registers (140 against 94)
+            const uint64_t e0 = m61::lmul(w[base + p], u[p]), e1 = m61::lmul(w[base + p], u[p + h]);
+            acc[3 * c] += m61::lmul(e0, v[p]);
+            acc[3 * c + 1] += m61::lmul(e1, v[p + h]);
+            acc[3 * c + 2] += m61::lmul(e0 + e1, v[p] + v[p + h]);
+            u[p] = fold(u[p], u[p + h], rho[c]);
+            v[p] = fold(v[p], v[p + h], rho[c]);
+            if ((p & 3) == 3 || p == h - 1) fold_all<3>(acc + 3 * c);
+        }
+    }
+}
+
 // R rounds j .. j + R - 1 over tables of 2^R q entries in one pass: a thread
-// holds the 2^R entries i + t q that end in entry i of the folded tables.  The
-// first pass reads the factors themselves.
-template <int R, bool FIRST>
-__device__ __forceinline__ void gate_pass_block(const GateArgs &a, int j, uint64_t q, int blk, int nblk, uint64_t *red)
+// holds the 2^R entries i + t q that end in entry i of the folded tables.
+template <int R>
+__global__ __launch_bounds__(256) void k_gate_pass(GateArgs a, int j, uint64_t q)
 {
     constexpr int NL = 1 << R;
-    uint64_t rho[R], rr[R], acc[3 * R];
+    __shared__ uint64_t red[m61::block_sum_words(3 * R, kThreads)];
+    uint64_t rho[R], rr[R], acc[3 * R] = {};
 #pragma unroll
     for (int c = 0; c < R; c++) {
         rho[c] = a.rho[j + c];
         rr[c] = a.r[j + c];
     }
-#pragma unroll
-    for (int c = 0; c < 3 * R; c++) acc[c] = 0;
-    const int nvar = a.lN - j - R;
-    for (uint64_t i = (uint64_t)blk * kThreads + threadIdx.x; i < q; i += (uint64_t)nblk * kThreads) {
+    for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < q; i += (uint64_t)gridDim.x * kThreads) {
         uint64_t u[NL], v[NL], w[NL];
-        int32_t ai[NL], bi[NL];
-        if (FIRST) {
-            gate_fetch<NL>(a.A, i, q, NL, a.lk, ai);
-            gate_fetch<NL>(a.B, i, q, NL, a.lk, bi);
 #pragma unroll
-            for (int t = 0; t < NL; t++) { u[t] = int_to_loose(ai[t]); v[t] = int_to_loose(bi[t]); }
-        } else {
-#pragma unroll
-            for (int t = 0; t < NL; t++) {
-                u[t] = a.T0[i + t * q];
-                v[t] = a.T1[i + t * q];
-            }
+        for (int t = 0; t < NL; t++) {
+            u[t] = a.T0[i + t * q];
+            v[t] = a.T1[i + t * q];
         }
-        x_weights<R>(suffix_weight(a.HS, a.LS, nvar, a.L, i), rr, w);
-#pragma unroll
-        for (int c = 0; c < R; c++) {
-            const int h = NL >> (c + 1), base = h - 1;
-#pragma unroll
-            for (int p = 0; p < h; p++) {
-                if (false) {
-                    rp_old(w[base + p], int_to_loose(ai[p]), int_to_loose(ai[p + h]), int_to_loose(bi[p]), int_to_loose(bi[p + h]), acc);
-                    u[p] = fold(int_to_loose(ai[p]), int_to_loose(ai[p + h]), rho[c]);
-                    v[p] = fold(int_to_loose(bi[p]), int_to_loose(bi[p + h]), rho[c]);
-                } else {
-                    rp_old(w[base + p], u[p], u[p + h], v[p], v[p + h], acc + 3 * c);
-                    u[p] = fold(u[p], u[p + h], rho[c]);
-                    v[p] = fold(v[p], v[p + h], rho[c]);
-                }
-                if ((p & 3) == 3 || p == h - 1) fold_all<3>(acc + 3 * c);  // pairs in order: their values need few registers
-            }
-        }
+        x_weights<R>(suffix_weight(a.HS, a.LS, a.lN - j - R, a.L, i), rr, w);
+        gate_rounds<R>(u, v, w, rho, acc);
         a.T0[i] = m61::canon(u[0]);
         a.T1[i] = m61::canon(v[0]);
     }
-    if (FIRST) ;  // U from the cross terms
     const uint64_t *t = m61::block_sum_lds<3 * R>(acc, red);
-    if (threadIdx.x < 3 * R)
-        a.part[(size_t)(3 * j + threadIdx.x) * kEntryMaxBlocks + blk] = t[threadIdx.x];
+    if (threadIdx.x < 3 * R) a.part[(size_t)(3 * j + threadIdx.x) * kEntryMaxBlocks + blockIdx.x] = t[threadIdx.x];
 }
 
-template <int R>
-__global__ __launch_bounds__(256) void k_gate_pass(GateArgs a, int j, uint64_t q)
+// The first R rounds, from the factors, and the product C of the same entries:
+// a thread's 2^R entries of C go out, with the witness where it is announced
+// (WIT; else the workgroup's extremes, as entries.hpp), while it works on its
+// field products, so that the stores (30 bytes an entry) and the products
+// overlap.  (Workgroups of their own for C beside those of the rounds did not:
+// 512 x 16384 entries took 92 us, 56 and 44 apart; so, 78.)
+// The claims' weights are eq(r, i + t q) = eq(r_0 .. r_{R-1}, t) eq(r_R .., i):
+// the 2^R first factors are the same for all threads, so sum_t of them times the
+// integers is exact in int64 by limbs (31 bits against Rm's 16, 21 against
+// Y's 31), and the second factor, the rounds' own, multiplies once.
+template <int R, bool WIT>
+__global__ __launch_bounds__(256, 3) void k_gate_first(GateArgs a, uint64_t q, EntriesArgs e)
 {
+    constexpr int NL = 1 << R;
     __shared__ uint64_t red[m61::block_sum_words(3 * R, kThreads)];
-    gate_pass_block<R, false>(a, j, q, blockIdx.x, gridDim.x, red);
-}
-
-// The first pass and the product (with the witness) side by side: the one
-// works on its field products, the other waits on memory.
-template <int R, int V, bool WIT>
-__global__ __launch_bounds__(256) void k_gate_first(GateArgs a, uint64_t q, int npass, EntriesArgs e)
-{
-    constexpr int W = m61::block_sum_words(3 * R, kThreads);
-    __shared__ uint64_t red[W > entries_lds_words(kThreads) ? W : entries_lds_words(kThreads)];
-    const int b = blockIdx.x, both = 2 * (npass < e.total ? npass : e.total);
-    const bool pass = b < both ? (b & 1) == 0 : npass > e.total;  // workgroup-uniform
-    const int idx = b < both ? b >> 1 : b - both / 2;
-    if (pass) {
-        gate_pass_block<R, true>(a, 0, q, idx, npass, red);
-        return;
+    uint64_t rho[R], rr[R], acc[3 * R] = {}, claims[2] = {};
+    int64_t lo = INT64_MAX, hi = INT64_MIN;
+    int oor = 0;
+#pragma unroll
+    for (int c = 0; c < R; c++) {
+        rho[c] = a.rho[c];
+        rr[c] = a.r[c];
     }
-    entries_block<V, WIT, kThreads, 1>(GateProduct<V>{a.A, a.B}, [&](uint64_t row) { return a.E1[row]; },
-                                    [&](uint64_t col) { return a.E2[col]; }, 1ull << (a.lN - a.lk), a.lk, e.C, e.we,
-                                    e.mm, idx, e.total, red);
+    int32_t km[NL][2], ky[NL][3];
+    if constexpr (WIT)
+#pragma unroll
+        for (int t = 0; t < NL; t++) {
+            uint64_t k = 1;
+#pragma unroll
+            for (int c = 0; c < R; c++) k = m61::lmul(k, (t >> (R - 1 - c)) & 1 ? rr[c] : m61::lsub(1, rr[c]));
+            k = m61::canon(k);
+            km[t][0] = __builtin_amdgcn_readfirstlane((int32_t)(k & 0x7FFFFFFF));
+            km[t][1] = __builtin_amdgcn_readfirstlane((int32_t)(k >> 31));
+#pragma unroll
+            for (int l = 0; l < 3; l++) ky[t][l] = __builtin_amdgcn_readfirstlane((int32_t)((k >> (21 * l)) & 0x1FFFFF));
+        }
+    for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < q; i += (uint64_t)gridDim.x * kThreads) {
+        int32_t ai[NL], bi[NL];
+        gate_fetch<NL>(a.A, i, q, NL, a.lk, ai);
+        gate_fetch<NL>(a.B, i, q, NL, a.lk, bi);
+        const uint64_t ei = suffix_weight(a.HS, a.LS, a.lN - R, a.L, i);
+        uint64_t sm[2] = {}, sy[3] = {};
+#pragma unroll
+        for (int t = 0; t < NL; t++) {
+            const int64_t c = (int64_t)ai[t] * bi[t];
+            const uint64_t x = i + t * q;
+            e.C[x] = c;
+            if constexpr (WIT) {
+                const WitOut o = witness_entry32(c, e.we.s, e.we.t, e.we.relu, e.we.half, oor);
+                e.we.R[x] = o.r;
+                e.we.Rm[x] = (uint16_t)o.rm;
+                e.we.Y[x] = o.y;
+                e.we.Z[x] = o.z;
+                e.we.bits[x] = o.w;
+#pragma unroll
+                for (int l = 0; l < 2; l++) sm[l] += (uint64_t)((int64_t)km[t][l] * o.rm);
+#pragma unroll
+                for (int l = 0; l < 3; l++) sy[l] += (uint64_t)((int64_t)ky[t][l] * o.y);
+            } else {
+                lo = c < lo ? c : lo;
+                hi = c > hi ? c : hi;
+            }
+        }
+        if constexpr (WIT) {
+            claims[0] = m61::lmacc(claims[0], m61::fold(m61::from_i64((int64_t)sm[0]) +
+                                                        m61::rotl(m61::from_i64((int64_t)sm[1]), 31)), ei);
+            claims[1] = m61::lmacc(claims[1], m61::fold(m61::from_i64((int64_t)sy[0]) +
+                                                        m61::rotl(m61::from_i64((int64_t)sy[1]), 21) +
+                                                        m61::rotl(m61::from_i64((int64_t)sy[2]), 42)), ei);
+        }
+        uint64_t u[NL], v[NL], w[NL];
+#pragma unroll
+        for (int t = 0; t < NL; t++) {
+            u[t] = int_to_loose(ai[t]);
+            v[t] = int_to_loose(bi[t]);
+        }
+        x_weights<R>(ei, rr, w);
+        gate_rounds<R>(u, v, w, rho, acc);
+        a.T0[i] = m61::canon(u[0]);
+        a.T1[i] = m61::canon(v[0]);
+    }
+    const uint64_t *t = m61::block_sum_lds<3 * R>(acc, red);
+    if (threadIdx.x < 3 * R) a.part[(size_t)threadIdx.x * kEntryMaxBlocks + blockIdx.x] = t[threadIdx.x];
+    __syncthreads();
+    if constexpr (WIT) entries_claims<kThreads>(claims, oor, e.we, blockIdx.x, red);
+    else entries_extremes<kThreads>(lo, hi, e.mm, blockIdx.x, red);
 }
 
 // Round j's value at X from its sums g = (Z_0, Z_1, U), lin = K_j eq1(r_j, X).
@@ -371,8 +414,8 @@ __global__ __launch_bounds__(kEntryTailThreads) void k_gate_tails(GateArgs a, in
 
 int gate_entries(const GateArgs &a, const EntriesArgs &e)
 {
-    const int V = entries_width(1ull << a.lk, e.C, e.wit ? &e.we : nullptr);
-    return entries_blocks(1ull << a.lN, V, entry_passes(a.lN) ? kThreads : kEntryTailThreads);
+    if (entry_passes(a.lN)) return entry_blocks(1ull << (a.lN - std::min(entry_pass_rounds(a.lN), kEntryPass)));
+    return entries_blocks(1ull << a.lN, entries_width(1ull << a.lk, e.C, e.wit ? &e.we : nullptr), kEntryTailThreads);
 }
 
 void launch_gate(const GateArgs &a, const EntriesArgs &e, hipStream_t st)
@@ -398,14 +441,15 @@ void launch_gate(const GateArgs &a, const EntriesArgs &e, hipStream_t st)
         const int nb = entry_blocks(q);
         const dim3 blk(kThreads);
         if (p == 0) {
-            entries_variant(1ull << a.lk, e, [&](auto Vc, auto Wc) {
-                constexpr int V = decltype(Vc)::value;
-                constexpr bool W = decltype(Wc)::value;
-                const dim3 grid(nb + e.total);
-                if (r == 3) hipLaunchKernelGGL((k_gate_first<3, V, W>), grid, blk, 0, st, a, q, nb, e);
-                else if (r == 2) hipLaunchKernelGGL((k_gate_first<2, V, W>), grid, blk, 0, st, a, q, nb, e);
-                else hipLaunchKernelGGL((k_gate_first<1, V, W>), grid, blk, 0, st, a, q, nb, e);
-            });
+#define RA_GATE_FIRST(R)                                                                                    \
+    do {                                                                                                    \
+        if (e.wit) hipLaunchKernelGGL((k_gate_first<R, true>), dim3(nb), blk, 0, st, a, q, e);              \
+        else hipLaunchKernelGGL((k_gate_first<R, false>), dim3(nb), blk, 0, st, a, q, e);                   \
+    } while (0)
+            if (r == 3) RA_GATE_FIRST(3);
+            else if (r == 2) RA_GATE_FIRST(2);
+            else RA_GATE_FIRST(1);
+#undef RA_GATE_FIRST
         } else if (r == 3) hipLaunchKernelGGL(k_gate_pass<3>, dim3(nb), blk, 0, st, a, j, q);
         else if (r == 2) hipLaunchKernelGGL(k_gate_pass<2>, dim3(nb), blk, 0, st, a, j, q);
         else hipLaunchKernelGGL(k_gate_pass<1>, dim3(nb), blk, 0, st, a, j, q);

@@ -342,3 +342,78 @@ def test_deferred_bad_token_is_reported_at_sync(ra):
     with pytest.raises(ra.RAError) as e:
         ctx.sync()
     assert e.value.code == -1
+
+
+def test_refused_layers_spend_their_announced_witness(ra):
+    """A witness announced for a layer whose product call is refused (a bad
+    token, a bad argument) is not made by the next layer: the announced buffers
+    stay as they are, and the next layer is the oracle's."""
+    rng = np.random.default_rng(17)
+    A, B = (ints(rng, s, np.int16, 300) for s in ((64, 64), (64, 64)))
+    E = dev(ints(rng, (50, 16), np.int16, 300))
+    chal = inputs.xorshift64_stream(89, 1000)
+    want = orc.prove_layer(A, B, 8, True, 0, chal, 0)
+    for refused in ("token", "argument"):
+        ctx, outs = ra.Context(chal), ra.witness_outputs(64, 64, "cuda")
+        for o in outs:
+            o.fill_(77)
+        ra.ra_witness_plan(ctx, 8, True, 0, want["t"], outs)
+        with pytest.raises(ra.RAError) as e:
+            if refused == "token":
+                ra.ra_embed_prove(ctx, dev(np.full(256, 50, dtype=np.int32)), E, 3)
+            else:
+                ra.ra_gate_prove(ctx, dev(A[:3]), dev(A[:3]))
+        assert e.value.code == -1 and ctx.cursor() == 0
+        torch.cuda.synchronize()
+        if refused == "token":  # that layer's own witness is in them; what counts is the next layer's
+            for o in outs:
+                o.fill_(77)
+        res = ra.prove_layer(ctx, dev(A), dev(B), 8, True, t=want["t"], plan=False)
+        same(res, want, EMBED)
+        assert all(bool((o == 77).all()) for o in outs)
+
+
+@pytest.mark.parametrize("n,k", [(1, 2), (64, 512), (128, 1024)])
+def test_gate_t_given_at_its_edge(ra, n, k):
+    """t given: the least t that holds R is taken, one less is refused, past
+    and below the 2^18 at which the claims' sums change (t = 17 and 18), and a
+    refused layer leaves the context usable for its witness alone."""
+    rng = np.random.default_rng(n)
+    chal = inputs.xorshift64_stream(97, 1000)
+    for bits in (11, 17, 18, 21, 28):
+        A = ints(rng, (n, k), np.int32, 1 << bits)
+        B = ints(rng, (n, k), np.int32, 16)
+        want = orc.prove_gate_layer(A, B, 4, False, 0, chal, 0)
+        t = want["t"]
+        same(ra.prove_gate(ra.Context(chal), dev(A), dev(B), 4, t=t), want, GATE)
+        with pytest.raises(ra.RAError) as e:
+            ra.prove_gate(ra.Context(chal), dev(A), dev(B), 4, t=t - 1)
+        assert e.value.code == -4
+
+
+def test_embed_wide_range(ra):
+    """R past 2^18 with t given (the claims' sums reduced a row at a time), many rows a thread."""
+    rng = np.random.default_rng(23)
+    n, vocab, d = 8192, 64, 256
+    tok, E = rng.integers(0, vocab, n).astype(np.int32), ints(rng, (vocab, d), np.int16, 1 << 15)
+    chal = inputs.xorshift64_stream(101, 1000)
+    want = orc.prove_embed_layer(tok, E, 2 ** 19 + 1, 6, False, 0, chal, 0)
+    assert want["t"] > 18
+    same(ra.prove_embed(ra.Context(chal), dev(tok), dev(E), 2 ** 19 + 1, 6, t=want["t"]), want, EMBED)
+
+
+def test_large_products_with_and_without_the_announcement(ra):
+    """2^22 outputs, where a thread takes four rows of an embedding at a time
+    and a gated product has four passes: the announced witness (made with the
+    product) and the witness call's own give the same proof and tables."""
+    rng = np.random.default_rng(29)
+    n, vocab, k = 8192, 999, 512
+    tok, E = dev(rng.integers(-1, vocab, n).astype(np.int32)), dev(ints(rng, (vocab, k - 3), np.int16, 1 << 11))
+    A, B = (dev(ints(rng, (n, k), np.int32, 1 << 12)) for _ in range(2))
+    got = []
+    for plan in (True, False):
+        ctx = ra.Context(seed=31)
+        got.append((ra.prove_embed(ctx, tok, E, 4000, 8, t=18, plan=plan), ra.prove_gate(ctx, A, B, 8, t=18, plan=plan)))
+    for x, y in zip(*got):
+        assert x["transcript"] == y["transcript"]
+        assert all(torch.equal(x[key], y[key]) for key in ("C", "R", "Rm", "Y", "Z", "bits"))
