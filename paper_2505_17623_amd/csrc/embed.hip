@@ -121,10 +121,12 @@ __device__ __forceinline__ uint64_t eq_prefix_sum(const uint64_t *r2, int lk, ui
     return m61::canon(sum);
 }
 
-// A workgroup takes 16 RT rows, each of its four waves every fourth chunk of
-// them; U chunks' loads are issued before the first is used.  Rows may start
-// at any even address; the last chunk of a width that is no multiple of 32 is
-// read entry by entry.
+// A workgroup takes 16 RT rows, each of its four waves a quarter of them; U
+// chunks' loads are issued before the first is used.  Rows may start at any
+// even address; the last chunk of a width that is no multiple of 32 is read
+// entry by entry.  What bounds it is the order in which memory is asked: with
+// the waves' chunks interleaved and a chunk's rows one after the other the same
+// loads took 204 us at 128000 x 4096 (1.05 GB), so 167 (6.3 TB/s).
 // The first ns workgroups scatter the tokens' weights.
 template <int RT, int U>
 __global__ __launch_bounds__(256) void k_embed_bind(EmbedArgs a_, int ns, uint64_t scale)
@@ -152,18 +154,21 @@ __global__ __launch_bounds__(256) void k_embed_bind(EmbedArgs a_, int ns, uint64
         acc[t] = none;
     }
     const v4i *col = limbs + 8 * g + (c & 7);
-    for (uint32_t q0 = wv; q0 < nq; q0 += 4 * U) {
+    // a wave's chunks are a quarter of the row in one piece, and a row's are asked
+    // for one after the other, so that memory sees 64 U bytes of a row at a time
+    const uint32_t per = (nq + 3) / 4, qe = (wv + 1) * per < nq ? (wv + 1) * per : nq;
+    for (uint32_t q0 = wv * per; q0 < qe; q0 += U) {
         v4i a[U][RT], w[U];
 #pragma unroll
-        for (int u = 0; u < U; u++) {
-            const uint32_t q = q0 + 4 * u < nq ? q0 + 4 * u : q0;  // wave-uniform
+        for (int u = 0; u < U; u++) w[u] = col[32 * (q0 + u < qe ? q0 + u : q0)];
 #pragma unroll
-            for (int t = 0; t < RT; t++) __builtin_memcpy(&a[u][t], row[t] + 32 * q, 16);
-            w[u] = col[32 * q];
-        }
+        for (int t = 0; t < RT; t++)
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                __builtin_memcpy(&a[u][t], row[t] + 32 * (q0 + u < qe ? q0 + u : q0), 16);
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            const v4i y = c < 8 && q0 + 4 * u < nq ? w[u] : none;
+            const v4i y = c < 8 && q0 + u < qe ? w[u] : none;
 #pragma unroll
             for (int t = 0; t < RT; t++)
                 acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u][t] ^ flip, y, acc[t], 0, 0, 0);
@@ -430,10 +435,11 @@ void launch_embed(const EmbedArgs &a, const EntriesArgs &e, hipStream_t st)
     const uint64_t threads = nl + (uint64_t)a.n + (1ull << a.lk);
     hipLaunchKernelGGL(k_embed_front, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, a, nl);
     const int ns = (int)((a.n + 255) / 256);
-    // 64 rows a workgroup use each fragment of the columns four times; 16 rows
-    // where 64 would leave CUs without a workgroup
-    if (a.rows >= 64 * 256)
-        hipLaunchKernelGGL((k_embed_bind<4, 4>), dim3(ns + (unsigned)(a.rows / 64)), dim3(256), 0, st, a, ns, scale);
+    // 32 rows a workgroup use each fragment of the columns twice (128000 x 4096:
+    // 167 us, with 16 rows 171); 16 rows where 32 would leave a CU fewer than two
+    // workgroups
+    if (a.rows >= 32 * 512)
+        hipLaunchKernelGGL((k_embed_bind<2, 8>), dim3(ns + (unsigned)(a.rows / 32)), dim3(256), 0, st, a, ns, scale);
     else
         hipLaunchKernelGGL((k_embed_bind<1, 8>), dim3(ns + (unsigned)((a.rows + 15) / 16)), dim3(256), 0, st, a, ns, scale);
     const int j0 = entry_pass_rounds(a.lv);
