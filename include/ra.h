@@ -16,6 +16,8 @@
  * Calling convention
  *   - Per layer: ra_sumcheck_matmul_prove, then ra_rescale_relu_witness,
  *     then ra_range_prove; layers in order.  Out of order -> RA_E_STATE.
+ *     A layer whose product is not a matrix's has ra_gate_prove or
+ *     ra_embed_prove in the first call's place.
  *   - Pointers named d_* are device pointers (caller-owned, on the device
  *     that was current when the context was created); h_* and the arrays
  *     inside the proof structs are host pointers (caller-owned).
@@ -335,8 +337,10 @@ ra_status ra_link_gather(ra_ctx *ctx, const int32_t *d_Z, uint64_t z_entries, co
 
 /* ---- Layers with another product than a matrix's ----------------------------
  * Two products of language models, each as a layer: its call stands in the
- * place of ra_sumcheck_matmul_prove (optionally after ra_witness_plan), and
- * the layer's ra_rescale_relu_witness and ra_range_prove follow as always.
+ * place of ra_sumcheck_matmul_prove, and the layer's ra_rescale_relu_witness
+ * (with d_C as this call left it) and ra_range_prove follow as always.
+ * ra_witness_plan works as before a matrix call; a call that is refused spends
+ * the plan too.
  * Over F_p only, as the gather links; a layer proven with them has no a* that
  * ra_link_prove could link (RA_E_STATE).  ra_verify_ops verifies them.
  *

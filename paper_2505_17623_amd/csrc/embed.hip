@@ -129,19 +129,19 @@ __device__ __forceinline__ uint64_t eq_prefix_sum(const uint64_t *r2, int lk, ui
 // loads took 204 us at 128000 x 4096 (1.05 GB), so 167 (6.3 TB/s).
 // The first ns workgroups scatter the tokens' weights.
 template <int RT, int U>
-__global__ __launch_bounds__(256) void k_embed_bind(EmbedArgs a_, int ns, uint64_t scale)
+__global__ __launch_bounds__(256) void k_embed_bind(EmbedArgs args, int ns, uint64_t scale)
 {
     __shared__ int32_t part[4][16 * RT][9];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, g = lane >> 4, c = lane & 15;
     if ((int)blockIdx.x < ns) {  // workgroup-uniform
-        embed_scatter(a_, a_.tr + 3 + 3 * (size_t)a_.lv, scale, (uint64_t)blockIdx.x * 256 + tid);
+        embed_scatter(args, args.tr + 3 + 3 * (size_t)args.lv, scale, (uint64_t)blockIdx.x * 256 + tid);
         return;
     }
-    const int16_t *__restrict__ E = a_.E;
-    const v4i *__restrict__ limbs = (const v4i *)a_.limbs;
-    const uint64_t ld = a_.ld, rows = a_.rows, *r2 = a_.r + a_.ln;
-    const uint32_t vocab = a_.vocab, d = a_.d;
-    const int lk = a_.lk;
+    const int16_t *__restrict__ E = args.E;
+    const v4i *__restrict__ limbs = (const v4i *)args.limbs;
+    const uint64_t ld = args.ld, rows = args.rows, *r2 = args.r + args.ln;
+    const uint32_t vocab = args.vocab, d = args.d;
+    const int lk = args.lk;
     const uint64_t v0 = (uint64_t)(blockIdx.x - ns) * (16 * RT);
     const uint32_t nq = d / 32;  // whole chunks
     const v4i flip{0x00800080, 0x00800080, 0x00800080, 0x00800080}, none{0, 0, 0, 0};
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256) void k_embed_bind(EmbedArgs a_, int ns, uint64
             s = m61::fold(s + m61::rotl(m61::from_i64(x), 8 * l));
         }
     }
-    a_.b[v0 + tid] = m61::canon(s);
+    args.b[v0 + tid] = m61::canon(s);
 }
 
 // V entries of C: scale times the token's row, zero past d, for token -1 and
