@@ -1911,9 +1911,10 @@ ra_status embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int1
         launch_embed(ea, en, c->stream);
     }
     begin_layer(c, n, k, need, en);
-    const ra_status r = finish(c, o_tr, [c, out, lv, need](const uint64_t *h) {
+    const uint64_t off = c->r12_off;
+    const ra_status r = finish(c, o_tr, [c, out, lv, need, off](const uint64_t *h) {
         if (h[3 + 3 * lv]) {  // a token outside [-1, vocab)
-            c->refused = need;
+            if (c->phase == 1 && c->r12_off == off) c->refused = need;  // found within its own layer
             return (ra_status)RA_E_INVAL;
         }
         out->log_m = (uint32_t)lv;

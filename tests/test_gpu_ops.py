@@ -344,6 +344,28 @@ def test_deferred_bad_token_is_reported_at_sync(ra):
     assert e.value.code == -1
 
 
+def test_deferred_bad_token_found_in_a_later_layer(ra):
+    """The first wait is a later layer's (its witness finds t): it reports the
+    refusal and is itself done, and the context goes on from there."""
+    rng = np.random.default_rng(18)
+    A, B = (ints(rng, s, np.int16, 300) for s in ((8, 16), (16, 8)))
+    chal = inputs.xorshift64_stream(91, 1000)
+    ctx = ra.Context(chal, deferred=True)
+    ra.prove_embed(ctx, dev(np.array([0, 99], dtype=np.int32)), dev(np.ones((10, 8), dtype=np.int16)), 3, 4, t=10)
+    start = ctx.cursor()
+    want = orc.prove_layer(A, B, 8, True, 0, chal, start)
+    C, mm = ra.ra_sumcheck_matmul_prove(ctx, dev(A), dev(B))
+    here, outs = ctx.cursor(), ra.witness_outputs(8, 8, "cuda")
+    assert here > start
+    with pytest.raises(ra.RAError) as e:
+        ra.ra_rescale_relu_witness(ctx, C, 8, True, outs=outs)
+    assert e.value.code == -1 and ctx.cursor() == here
+    R, _, Y, _, bits = outs
+    rg = ra.ra_range_prove(ctx, bits, R, Y, ra.WitnessInfo(s=8, relu=1, round_mode=0, t=want["t"], P=want["P"]))
+    ctx.sync()
+    assert mm["mm_evals"] == want["mm_evals"] and rg["rs_evals"] == want["rs_evals"]
+
+
 def test_refused_layers_spend_their_announced_witness(ra):
     """A witness announced for a layer whose product call is refused (a bad
     token, a bad argument) is not made by the next layer: the announced buffers
