@@ -86,8 +86,9 @@ template <int V> struct GateProduct {
     }
 };
 
-// The suffix eq tables of r and the prefix products K_j (xsetup.hpp) by the
-// first nx threads, the eq tables E1 (r1) and E2 (r2) by the others.
+// The suffix eq tables of r (xsetup.hpp, whose prefix products K_j the tails
+// make for themselves) by the first nx threads, the eq tables E1 (r1) and E2
+// (r2) by the others.
 __global__ __launch_bounds__(256) void k_gate_setup(XSetupArgs a, int nx, int ln, uint64_t *E1, uint64_t *E2)
 {
     __shared__ uint64_t rl[64], sl[64];
@@ -106,14 +107,6 @@ __global__ __launch_bounds__(256) void k_gate_setup(XSetupArgs a, int nx, int ln
     else if (i - n < 1ull << (a.lN - ln)) E2[i - n] = eq_suffix(rl, ln, a.lN - ln, i - n);
 }
 
-
-__device__ __forceinline__ void rp_old(uint64_t w, uint64_t d0, uint64_t d1, uint64_t s0, uint64_t s1, uint64_t *acc)
-{
-    const uint64_t ed0 = m61::lmul(w, d0), ed1 = m61::lmul(w, d1);
-    acc[0] += m61::lmul(ed0, s0);
-    acc[1] += m61::lmul(ed1, s1);
-    acc[2] += m61::lmul(ed0 + ed1, s0 + s1);
-}
 // C rounds of one sub-cube held in registers (u, v folded or loose), weights w
 // (x_weights): round c's sums added to acc[3 c ..], folded every fourth pair.
 template <int R>
