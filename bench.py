@@ -159,8 +159,8 @@ def traffic_file(cfg):
 # the sources of the kernels a headline step launches (the F_p path) and of
 # their launchers: counters taken on other versions of these are stale
 HEADLINE_SOURCES = ["witness.hip", "gemm.hip", "sumcheck.hip", "planes.hip", "xrounds.hip", "m61.hpp",
-                    "common.hpp", "gram_reduce.hpp", "plane_round.hpp", "xsetup.hpp", "assemble.hpp", "claims.hpp",
-                    "tail.hpp", "rsetup.hpp"]
+                    "common.hpp", "gram_reduce.hpp", "plane_round.hpp", "xsetup.hpp", "xpair.hpp", "assemble.hpp",
+                    "claims.hpp", "tail.hpp", "rsetup.hpp"]
 
 
 def sources_digest():
