@@ -21,6 +21,7 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v16i __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 64;    // block tile (rows and columns)
+constexpr int kRowsMax = 32, kRowsCols = 32;  // k_gemm_rows: rows at most, columns a workgroup
 // LDS stages (k steps of 64) per block: 48 KB for int16 A (three blocks fit
 // a CU, so the matrix tail's workgroup runs beside two tiles per CU), 72 KB
 // for int32 A.  A fourth stage for int16 A was slower.
@@ -767,6 +768,143 @@ __global__ __launch_bounds__(256, 2) void k_gemm_mfma(const int8_t *__restrict__
     }
 }
 
+// The product for at most 32 rows (a single token's layer), where the 64 x 64
+// tiles are few and half empty: a workgroup takes 32 columns, its four waves a
+// quarter of the inner dimension each, straight from memory into registers (no
+// wave's fragments are another's), and their sums meet in LDS as int64.  What
+// bounds it is what one CU can read: 1 x 4096 x 1024 (int32 A, four limbs) 18
+// us against 37 with a CU's 64 steps one after the other.  Rows past n read row
+// 0's limbs; their sums are not used.  Witness and tail workgroups as in
+// k_gemm_mfma.
+template <int LA, int LE>
+__device__ __forceinline__ void rows_loop(const int8_t *__restrict__ a0, const int8_t *__restrict__ b0, size_t pa,
+                                          size_t pb, uint32_t q0, uint32_t q1, v16i (&acc)[LA == 2 ? 4 : LA + 1])
+{
+    constexpr int U = 8;  // chunks of 32 in flight: up to 48 loads of 16 bytes a lane
+    for (uint32_t q = q0; q < q1; q += U) {
+        v4i a[U][LE], b[U][2];
+#pragma unroll
+        for (int e = 0; e < U; e++) {
+            const size_t x = (size_t)(q + e < q1 ? q + e : q) * 1024;
+#pragma unroll
+            for (int u = 0; u < LE; u++) a[e][u] = *(const v4i *)(a0 + u * pa + x);
+#pragma unroll
+            for (int v = 0; v < 2; v++) b[e][v] = *(const v4i *)(b0 + v * pb + x);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // all loads go out before the first product
+#pragma unroll
+        for (int e = 0; e < U; e++) {
+            if (q + e >= q1) b[e][0] = b[e][1] = v4i{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 2 * LE; i++) {  // in gemm_loop's order
+                const int u = LE == 3 ? (i < 3 ? i : i == 3 ? 2 : i - 4) : i % LE;
+                const int v = LE == 3 ? (i >= 3) : i / LE;
+                const int w = LA == 2 ? 2 * u + v : u + v;
+                acc[w] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[e][u], b[e][v], acc[w], 0, 0, 0);
+            }
+        }
+    }
+}
+
+template <int LA, bool WIT>
+__global__ __launch_bounds__(256, 1) void k_gemm_rows(const int8_t *__restrict__ Al, const int8_t *__restrict__ Bt,
+                                                   const int64_t *__restrict__ rowsum,
+                                                   const int32_t *__restrict__ rowlimb,
+                                                   const int64_t *__restrict__ colpart, int ntiles, uint32_t n,
+                                                   uint32_t m, uint32_t k, uint32_t np, uint32_t mp, uint32_t kp,
+                                                   int64_t *__restrict__ C, TailArgs ta, XJobs jobs, WitEpi we)
+{
+    constexpr int NC = kRowsCols;
+    static_assert(NC * kRowsMax + NC + m61::block_sum_words(3, 256) <= kTailSmem, "sums beside the claims' area");
+    __shared__ __attribute__((aligned(16))) uint64_t smem[kTailSmem];
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const uint32_t nblk = (k + NC - 1) / NC;
+    if (blockIdx.x >= nblk) {  // workgroup-uniform
+        tail_block<KIND_MATMUL>(ta, jobs, (int)(blockIdx.x - nblk), smem);
+        return;
+    }
+    uint64_t *sum = smem, *cs = smem + NC * kRowsMax, *red = cs + NC;
+    for (int i = tid; i < NC * kRowsMax + NC; i += 256) sum[i] = 0;
+    // thread t: column t mod 32 of rows t / 32 + 8 e, and of an eighth of the column sums' tiles
+    constexpr int RT = kRowsMax / 8;
+    const uint32_t bj = blockIdx.x, col = bj * NC + (tid & (NC - 1)), r0 = tid / NC;
+    const bool in = col < k;
+    int64_t c8 = 0, rs[RT] = {};
+    uint64_t e1[RT] = {}, e2 = 0;
+    int rl = 3;
+    if (in)
+        for (int t = (int)r0; t < ntiles; t += 8) c8 += colpart[(size_t)t * kp + col];
+#pragma unroll
+    for (int e = 0; e < RT; e++)
+        if (r0 + 8 * e < n) {
+            rs[e] = rowsum[r0 + 8 * e];
+            if (WIT) e1[e] = we.E1[r0 + 8 * e];
+        }
+    if (WIT && in) e2 = we.E2[col];
+    if (LA == 4 && tid < (int)n) rl = rowlimb[tid];
+    constexpr int NACC = LA == 2 ? 4 : LA + 1;
+    v16i acc[NACC];
+#pragma unroll
+    for (int w = 0; w < NACC; w++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) acc[w][r] = 0;
+    const uint32_t nR = np >> 5, nC = kp >> 5, nQ = mp >> 5, per = (nQ + 3) / 4;
+    const uint32_t q0 = wv * per, q1 = q0 + per < nQ ? q0 + per : nQ;
+    const int8_t *a0 = Al + 16 * ((uint32_t)(lane & 31) < n ? lane : lane & 32);
+    const int8_t *b0 = Bt + frag_off(0, bj, 0, nC, nQ) + 16 * lane;
+    const size_t pa = frag_off(1, 0, 0, nR, nQ), pb = frag_off(1, 0, 0, nC, nQ);
+    const bool four = __syncthreads_or(rl > 3);  // and the sums are cleared
+    if (LA == 2) rows_loop<LA, 2>(a0, b0, pa, pb, q0, q1, acc);
+    else if (four) rows_loop<LA, LA>(a0, b0, pa, pb, q0, q1, acc);
+    else rows_loop<LA, LA == 2 ? 2 : 3>(a0, b0, pa, pb, q0, q1, acc);
+    if (c8) atomicAdd((unsigned long long *)&cs[tid & (NC - 1)], (unsigned long long)c8);
+#pragma unroll
+    for (int r = 0; r < 16; r++) {
+        const uint32_t row = 8 * (r / 4) + 4 * (lane >> 5) + (r % 4);
+        uint64_t c = 0;
+#pragma unroll
+        for (int w = 0; w < NACC; w++) {
+            const int wt = LA == 2 ? (w >> 1) + (w & 1) : w;  // weight 256^wt
+            c += (uint64_t)(int64_t)acc[w][r] << (8 * wt);
+        }
+        if (row < n) atomicAdd((unsigned long long *)&sum[row * NC + (lane & 31)], (unsigned long long)c);
+    }
+    __syncthreads();
+    // recombination as in k_gemm_mfma
+    constexpr int64_t cA = LA == 2 ? 128 : 128 + 128 * 256 + 128 * 65536;
+    const uint64_t corr = (uint64_t)cA * cs[tid & (NC - 1)] - (uint64_t)(128 * cA) * m;
+    uint64_t claims[3] = {0, 0, 0};
+    int oor = 0;
+#pragma unroll
+    for (int e = 0; e < RT; e++) {
+        const uint32_t row = r0 + 8 * e;
+        if (row >= n || !in) continue;
+        const uint64_t c = sum[row * NC + (tid & (NC - 1))] + corr + 128 * (uint64_t)rs[e];
+        const size_t x = (size_t)row * k + col;
+        C[x] = (int64_t)c;
+        if (!WIT) continue;
+        const WitOut o = witness_entry((int64_t)c, we.s, we.t, we.relu, we.half, oor);
+        we.R[x] = o.r;
+        we.Rm[x] = (uint16_t)o.rm;
+        we.Y[x] = o.y;
+        we.Z[x] = o.z;
+        we.bits[x] = o.w;
+        const uint64_t w = m61::lmul(e1[e], e2);
+        claims[0] = m61::lmacc(claims[0], m61::from_i64(o.r), w);
+        claims[1] = m61::lmacc(claims[1], m61::from_i64(o.rm), w);
+        claims[2] = m61::lmacc(claims[2], m61::from_i64(o.y), w);
+    }
+    if (!WIT) return;
+    const int any = __syncthreads_or(oor);
+    const uint64_t *t = m61::block_sum_lds<3>(claims, red);
+    if (tid != 0) return;
+    uint64_t *part = we.claim_part + 4 * (size_t)blockIdx.x;
+#pragma unroll
+    for (int q = 0; q < 3; q++) part[q] = t[q];
+    part[3] = we.relu ? m61::rotl(m61::add(t[0], t[2]), 60) : t[0];  // 2^60 = 1/2
+    we.flags[blockIdx.x] = (uint32_t)any;
+}
+
 size_t gemm_workspace_bytes(int a_is_i32, uint32_t n, uint32_t m, uint32_t k)
 {
     const size_t np = round_up64(n), mp = round_up64(m), kp = round_up64(k);
@@ -859,7 +997,18 @@ void launch_front(const void *A, int a_is_i32, const int16_t *B, uint32_t n, uin
     }
 }
 
-uint32_t gemm_tiles(uint32_t n, uint32_t k) { return (round_up64(k) / kTile) * (round_up64(n) / kTile); }
+// k_gemm_rows to 32 rows and 128 workgroups, where it was never slower (launch
+// with its tail, the tiles against it, us: 1 x 64 x 64 10.0 / 8.2, 1 x 1024 x
+// 4096 14.5 / 11.6, 1 x 4096 x 1024 27 / 16 and with int32 A 33 / 18, 32 x 4096
+// x 4096 29 / 19, 1 x 32768 x 1024 155 / 73).  With one for every CU the tail,
+// which an int32 A leaves no room beside, has to wait: 1 x 64 x 8192 10 / 14.
+static bool gemm_by_rows(uint32_t n, uint32_t k) { return n <= (uint32_t)kRowsMax && k <= 128u * kRowsCols; }
+
+uint32_t gemm_tiles(uint32_t n, uint32_t k)
+{
+    if (gemm_by_rows(n, k)) return (k + kRowsCols - 1) / kRowsCols;
+    return (round_up64(k) / kTile) * (round_up64(n) / kTile);
+}
 
 void launch_gemm_mfma(const void *A, int a_is_i32, const int16_t *B, int64_t *C, uint32_t n, uint32_t m, uint32_t k,
                       void *ws, hipStream_t st, const TailArgs *ta, const XJobs *jobs, bool split_done,
@@ -881,15 +1030,17 @@ void launch_gemm_mfma(const void *A, int a_is_i32, const int16_t *B, int64_t *C,
     const TailArgs tnone{};
     XJobs jnone{};
     const uint32_t extra = ta ? 1u + (uint32_t)jobs->nslot : 0u;
-    const dim3 grid((kp / kTile) * (np / kTile) + extra);
+    const dim3 grid(gemm_tiles(n, k) + extra);
+    const bool rows = gemm_by_rows(n, k);
     const TailArgs &tav = ta ? *ta : tnone;
     const XJobs &jv = ta ? *jobs : jnone;
     const WitEpi wnone{};
     const WitEpi &wv = we ? *we : wnone;
 #define RA_GEMM(LAV, W)                                                                                            \
-    hipLaunchKernelGGL((k_gemm_mfma<LAV, gemm_stages<LAV>(), W>), grid, dim3(256), 0, st, (const int8_t *)w.Al,    \
-                       (const int8_t *)w.Bt, (const int64_t *)w.rowsum, (const int32_t *)w.rowlimb,                \
-                       (const int64_t *)w.colpart, ntiles, n, m, k, np, mp, kp, C, tav, jv, wv)
+    hipLaunchKernelGGL((rows ? k_gemm_rows<LAV, W> : k_gemm_mfma<LAV, gemm_stages<LAV>(), W>), grid, dim3(256), 0, \
+                       st, (const int8_t *)w.Al, (const int8_t *)w.Bt, (const int64_t *)w.rowsum,                  \
+                       (const int32_t *)w.rowlimb, (const int64_t *)w.colpart, ntiles, n, m, k, np, mp, kp, C,     \
+                       tav, jv, wv)
     if (a_is_i32) {
         if (we) RA_GEMM(4, true);
         else RA_GEMM(4, false);

@@ -439,3 +439,24 @@ def test_large_products_with_and_without_the_announcement(ra):
     for x, y in zip(*got):
         assert x["transcript"] == y["transcript"]
         assert all(torch.equal(x[key], y[key]) for key in ("C", "R", "Rm", "Y", "Z", "bits"))
+
+
+@pytest.mark.parametrize("n,m,k", [(1, 1, 1), (1, 64, 8), (1, 4096, 64), (2, 2048, 256), (8, 32, 32), (32, 512, 128),
+                                   (2, 64, 4096), (2, 64, 8192), (1, 128, 16384),
+                                   (64, 64, 64)])
+@pytest.mark.parametrize("kind", ["int16", "int32", "int24"])
+def test_matrix_layers_of_few_rows(ra, n, m, k, kind):
+    """A block's projections for few tokens: the inner dimension split in a
+    workgroup (to 32 rows and 4096 columns), beside sizes past that; int32
+    inputs with four limbs and with three; t found, given and announced."""
+    rng = np.random.default_rng(n + m + k)
+    A = ints(rng, (n, m), np.int16, 2000) if kind == "int16" else \
+        ints(rng, (n, m), np.int32, 1 << 20) if kind == "int32" else np.abs(ints(rng, (n, m), np.int32, 1 << 20))
+    A.flat[0] = {"int16": -2000, "int32": -(1 << 24), "int24": (1 << 24) - 1}[kind]
+    B = ints(rng, (m, k), np.int16, 300)
+    chal = inputs.xorshift64_stream(93, 1000)
+    for relu, mode in ((True, 0), (False, 1)):
+        want = orc.prove_layer(A, B, 12, relu, mode, chal, 0)
+        for t, plan in ((-1, False), (want["t"], False), (want["t"], True)):
+            ctx = ra.Context(chal)
+            same(ra.prove_layer(ctx, dev(A), dev(B), 12, relu, mode, t, plan=plan), want, EMBED)
