@@ -651,16 +651,28 @@ def prove_gated_ffn(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.T
             bufs.append({})
     t = [-1] * count if ts is None else [int(x) for x in ts]
     b = [None] * count if bufs is None else bufs
-    gate = prove_layer(ctx, X, Wg, s, gate_relu, mode, t[0], b[0], plan, ws)
-    up = prove_layer(ctx, X, Wu, s, False, mode, t[1], b[1], plan, ws)
-    mid = prove_gate(ctx, gate["Z"], up["Z"], s, False, mode, t[2], b[2], plan, ws)
+    # without ts each witness call waits for its t, and that wait completes the
+    # calls before it: one wait a layer and one at the end (64 tokens, 256 -> 683
+    # -> 256: 383 -> 351 us; one token, 1024 -> 2730 -> 1024: 398 -> 360)
+    join = ts is None and not ctx.deferred
+    if join:
+        ctx.set_deferred(True)
+    try:
+        gate = prove_layer(ctx, X, Wg, s, gate_relu, mode, t[0], b[0], plan, ws)
+        up = prove_layer(ctx, X, Wu, s, False, mode, t[1], b[1], plan, ws)
+        mid = prove_gate(ctx, gate["Z"], up["Z"], s, False, mode, t[2], b[2], plan, ws)
+        res = [gate, up, mid]
+        if Wd is not None:
+            res.append(prove_layer(ctx, mid["Z"], Wd, s, False, mode, t[3], b[3], plan, ws))
+            res[3]["A"] = mid["Z"]
+        if join:
+            ctx.sync()
+    finally:
+        if join:
+            ctx.set_deferred(False)
     gate["A"] = up["A"] = X
     mid["A"], mid["B"] = gate["Z"], up["Z"]
-    if Wd is None:
-        return [gate, up, mid]
-    down = prove_layer(ctx, mid["Z"], Wd, s, False, mode, t[3], b[3], plan, ws)
-    down["A"] = mid["Z"]
-    return [gate, up, mid, down]
+    return res
 
 
 def to_device(a: np.ndarray, device="cuda"):

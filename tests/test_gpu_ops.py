@@ -460,3 +460,46 @@ def test_matrix_layers_of_few_rows(ra, n, m, k, kind):
         for t, plan in ((-1, False), (want["t"], False), (want["t"], True)):
             ctx = ra.Context(chal)
             same(ra.prove_layer(ctx, dev(A), dev(B), 12, relu, mode, t, plan=plan), want, EMBED)
+
+
+def test_gated_block_refused_leaves_the_context_as_its_calls_do(ra):
+    """A block whose gated product has t = 39 (R past int32: not implemented): the refusal, the
+    mode and the position are those of the same calls made one by one."""
+    rng = np.random.default_rng(19)
+    X = ints(rng, (8, 64), np.int32, 1 << 21)
+    Wg, Wu = (ints(rng, (64, 32), np.int16, 300) for _ in range(2))
+    one, block = ra.Context(seed=8), ra.Context(seed=8)
+    gate = ra.prove_layer(one, dev(X), dev(Wg), 8, True)
+    up = ra.prove_layer(one, dev(X), dev(Wu), 8, False)
+    codes = []
+    for call in (lambda: ra.prove_gate(one, gate["Z"], up["Z"], 8),
+                 lambda: ra.prove_gated_ffn(block, dev(X), dev(Wg), dev(Wu), 8)):
+        with pytest.raises(ra.RAError) as e:
+            call()
+        codes.append(e.value.code)
+    assert codes == [-9, -9] and not block.deferred and one.cursor() == block.cursor()
+    for ctx in (one, block):  # the layer waits for its witness, as after any refused range
+        with pytest.raises(ra.RAError) as e:
+            ra.prove_gate(ctx, gate["Z"], up["Z"], 8)
+        assert e.value.code == -7
+
+
+@pytest.mark.parametrize("down", [False, True])
+def test_gated_block_without_t_equals_its_calls(ra, down):
+    """t found: the block, which waits once a layer, and its calls one by one, twice in a row."""
+    rng = np.random.default_rng(20)
+    X = ints(rng, (8, 64), np.int16, 500)
+    Wg, Wu = (ints(rng, (64, 128), np.int16, 60) for _ in range(2))
+    Wd = dev(ints(rng, (128, 64), np.int16, 60)) if down else None
+    X, Wg, Wu = dev(X), dev(Wg), dev(Wu)
+    one, block = ra.Context(seed=9), ra.Context(seed=9)
+    for _ in range(2):
+        gate, up = ra.prove_layer(one, X, Wg, 8, True), ra.prove_layer(one, X, Wu, 8, False)
+        want = [gate, up, ra.prove_gate(one, gate["Z"], up["Z"], 8)]
+        if down:
+            want.append(ra.prove_layer(one, want[2]["Z"], Wd, 8, False))
+        got = ra.prove_gated_ffn(block, X, Wg, Wu, 8, Wd=Wd)
+        assert not block.deferred and one.cursor() == block.cursor() and len(got) == len(want)
+        for x, y in zip(got, want):
+            assert x["transcript"] == y["transcript"] and x["transcript"]["rs_evals"]
+            assert all(torch.equal(x[key], y[key]) for key in ("C", "R", "Rm", "Y", "Z", "bits"))
