@@ -653,7 +653,7 @@ def prove_gated_ffn(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.T
     b = [None] * count if bufs is None else bufs
     # without ts each witness call waits for its t, and that wait completes the
     # calls before it: one wait a layer and one at the end (64 tokens, 256 -> 683
-    # -> 256: 383 -> 351 us; one token, 1024 -> 2730 -> 1024: 398 -> 360)
+    # -> 256: 383 -> 352 us; one token, 1024 -> 2730 -> 1024: 398 -> 363)
     join = ts is None and not ctx.deferred
     if join:
         ctx.set_deferred(True)
