@@ -37,7 +37,8 @@
  *     before column bits (worked example of Sec. III-A-1).
  *   - Every function returns RA_OK (0) or a negative ra_status; none throws
  *     or aborts.  After an error the context is left in its previous state
- *     unless the error is RA_E_HIP.
+ *     (but for an announced witness, see ra_witness_plan) unless the error is
+ *     RA_E_HIP.
  */
 #ifndef RA_H
 #define RA_H
@@ -256,8 +257,11 @@ ra_status ra_rescale_relu_witness(ra_ctx *ctx, const int64_t *d_C, uint32_t n, u
  * The witness call then only sums its claims if its arguments are exactly
  * these (and bits_words covers n * k); any other witness call, or a product
  * the fusion does not take, runs the witness in full, so the results never
- * depend on the plan.  The plan is used by one layer.
- * Errors: RA_E_INVAL for a null buffer, t < 0 or parameters the witness call
+ * depend on the plan.  The plan is used by one layer: the next product call
+ * (ra_sumcheck_matmul_prove, ra_gate_prove, ra_embed_prove) spends it, also one
+ * that is refused.  All five buffers null withdraws it, for a caller that
+ * gives the layer up before its product call.
+ * Errors: RA_E_INVAL for a null buffer among others, t < 0 or parameters the witness call
  * would reject; RA_E_FIELD_TOO_SMALL / RA_E_NOT_IMPLEMENTED as that call
  * would return them for s and t; RA_E_STATE when called between a layer's
  * calls. */
@@ -339,8 +343,7 @@ ra_status ra_link_gather(ra_ctx *ctx, const int32_t *d_Z, uint64_t z_entries, co
  * Two products of language models, each as a layer: its call stands in the
  * place of ra_sumcheck_matmul_prove, and the layer's ra_rescale_relu_witness
  * (with d_C as this call left it) and ra_range_prove follow as always.
- * ra_witness_plan works as before a matrix call; a call that is refused spends
- * the plan too.
+ * ra_witness_plan works as before a matrix call.
  * Over F_p only, as the gather links; a layer proven with them has no a* that
  * ra_link_prove could link (RA_E_STATE).  ra_verify_ops verifies them.
  *

@@ -339,6 +339,17 @@ void take_back(ra_ctx *c)
     c->plan.valid = c->plan.fused = false;
 }
 
+// A product call that is refused leaves the context between layers, and spends
+// an announced witness as one that runs does: the layer that it was announced
+// for may never come, and its buffers may not outlive the call.
+struct SpendsPlan {
+    ra_ctx *c;
+    ~SpendsPlan()
+    {
+        if (c->phase == 0) c->plan.valid = c->plan.fused = false;
+    }
+};
+
 // Plane count of the bit table for given s, t, relu (the rule of the witness
 // kernel, Sec. III-A-2 and III-B): s + (t + 2) (1 + relu) planes, rounded up to
 // a power of two.
@@ -754,7 +765,9 @@ ra_status ra_sumcheck_matmul_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype,
                                    uint32_t m, uint32_t k, int64_t *d_C, void *d_ws, size_t ws_bytes,
                                    ra_matmul_proof *out)
 {
-    if (!c || !d_A || !d_B || !d_C || !out) return RA_E_INVAL;
+    if (!c) return RA_E_INVAL;
+    const SpendsPlan spends{c};
+    if (!d_A || !d_B || !d_C || !out) return RA_E_INVAL;
     if (!is_pow2(n) || !is_pow2(m) || !is_pow2(k)) return RA_E_INVAL;
     if (a_dtype != RA_I16 && a_dtype != RA_I32) return RA_E_INVAL;
     if (m > kGemmMaxInner) return RA_E_NOT_IMPLEMENTED;  // exactness of the limb products
@@ -854,7 +867,13 @@ ra_status ra_sumcheck_matmul_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype,
 ra_status ra_witness_plan(ra_ctx *c, uint32_t s, uint32_t relu, uint32_t round_mode, int32_t t, int32_t *d_R,
                           uint16_t *d_Rm, int32_t *d_Y, int32_t *d_Z, uint64_t *d_bits, uint64_t bits_words)
 {
-    if (!c || !d_R || !d_Rm || !d_Y || !d_Z || !d_bits) return RA_E_INVAL;
+    if (!c) return RA_E_INVAL;
+    if (!d_R && !d_Rm && !d_Y && !d_Z && !d_bits) {  // withdrawn
+        if (c->phase != 0) return RA_E_STATE;
+        c->plan.valid = c->plan.fused = false;
+        return RA_OK;
+    }
+    if (!d_R || !d_Rm || !d_Y || !d_Z || !d_bits) return RA_E_INVAL;
     if (c->phase != 0) return RA_E_STATE;
     if (s < 1 || relu > 1 || round_mode > 1 || t < 0) return RA_E_INVAL;
     if (s > 16) return RA_E_NOT_IMPLEMENTED;  // Rm is uint16
@@ -1774,11 +1793,12 @@ extern "C" ra_status ra_gate_workspace_size(uint32_t n, uint32_t k, size_t *byte
     return RA_OK;
 }
 
-namespace {
-ra_status gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype, uint64_t lda, const void *d_B,
-                     ra_dtype b_dtype, uint64_t ldb, uint32_t n, uint32_t k, int64_t *d_C, void *d_ws, size_t ws_bytes,
-                     ra_gate_proof *out)
+extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype, uint64_t lda, const void *d_B,
+                                   ra_dtype b_dtype, uint64_t ldb, uint32_t n, uint32_t k, int64_t *d_C, void *d_ws,
+                                   size_t ws_bytes, ra_gate_proof *out)
 {
+    if (!c) return RA_E_INVAL;
+    const SpendsPlan spends{c};
     if (!d_A || !d_B || !d_C || !out) return RA_E_INVAL;
     if (!is_pow2(n) || !is_pow2(k)) return RA_E_INVAL;
     if ((a_dtype != RA_I16 && a_dtype != RA_I32) || (b_dtype != RA_I16 && b_dtype != RA_I32)) return RA_E_INVAL;
@@ -1833,20 +1853,6 @@ ra_status gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype, uint64_t lda,
     });
 }
 
-}  // namespace
-
-// A call that is refused spends an announced witness too: its buffers may not
-// outlive the call.
-extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype, uint64_t lda, const void *d_B,
-                                   ra_dtype b_dtype, uint64_t ldb, uint32_t n, uint32_t k, int64_t *d_C, void *d_ws,
-                                   size_t ws_bytes, ra_gate_proof *out)
-{
-    if (!c) return RA_E_INVAL;
-    const ra_status st = gate_prove(c, d_A, a_dtype, lda, d_B, b_dtype, ldb, n, k, d_C, d_ws, ws_bytes, out);
-    if (st != RA_OK && c->phase == 0) c->plan.valid = false;
-    return st;
-}
-
 extern "C" ra_status ra_embed_workspace_size(uint32_t n, uint32_t vocab, uint32_t d, size_t *bytes)
 {
     if (!bytes || !is_pow2(n) || !vocab || !d) return RA_E_INVAL;
@@ -1857,10 +1863,12 @@ extern "C" ra_status ra_embed_workspace_size(uint32_t n, uint32_t vocab, uint32_
     return RA_OK;
 }
 
-namespace {
-ra_status embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde, uint32_t vocab,
-                      uint32_t d, int32_t scale, int64_t *d_C, void *d_ws, size_t ws_bytes, ra_matmul_proof *out)
+extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde,
+                                    uint32_t vocab, uint32_t d, int32_t scale, int64_t *d_C, void *d_ws,
+                                    size_t ws_bytes, ra_matmul_proof *out)
 {
+    if (!c) return RA_E_INVAL;
+    const SpendsPlan spends{c};
     if (!d_tokens || !d_E || !d_C || !out) return RA_E_INVAL;
     if (!is_pow2(n) || !vocab || !d || lde < d) return RA_E_INVAL;
     if (vocab > kEmbedMaxVocab || d > kEmbedMaxWidth) return RA_E_NOT_IMPLEMENTED;
@@ -1926,18 +1934,6 @@ ra_status embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int1
     });
     take_back(c);
     return r;
-}
-
-}  // namespace
-
-extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t n, const int16_t *d_E, uint64_t lde,
-                                    uint32_t vocab, uint32_t d, int32_t scale, int64_t *d_C, void *d_ws,
-                                    size_t ws_bytes, ra_matmul_proof *out)
-{
-    if (!c) return RA_E_INVAL;
-    const ra_status st = embed_prove(c, d_tokens, n, d_E, lde, vocab, d, scale, d_C, d_ws, ws_bytes, out);
-    if (st != RA_OK && c->phase == 0) c->plan.valid = false;
-    return st;
 }
 
 // ---------------------------------------------------------------------------

@@ -9,6 +9,7 @@ raises, there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -348,6 +349,21 @@ def _ws(ws):
     return ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size()
 
 
+def _spends_plan(f):
+    """For a function that makes a layer's product call: an announced witness
+    is spent also when it raises before that call (which spends it, refused or
+    not), since the announced outputs may be freed or used otherwise next."""
+    @functools.wraps(f)
+    def call(ctx, *args, **kwargs):
+        try:
+            return f(ctx, *args, **kwargs)
+        except BaseException:
+            lib().ra_witness_plan(ctx.h, 0, 0, 0, -1, None, None, None, None, None, 0)
+            raise
+    return call
+
+
+@_spends_plan
 def ra_sumcheck_matmul_prove(ctx: Context, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor | None = None,
                              ws: torch.Tensor | None = None):
     """Returns (C, transcript dict); in deferred mode the dict is filled at ctx.sync().
@@ -425,6 +441,7 @@ def ra_range_prove(ctx: Context, bits, R, Y, info: WitnessInfo, ws: torch.Tensor
     return res
 
 
+@_spends_plan
 def prove_layer(ctx: Context, A: torch.Tensor, B: torch.Tensor, s: int, relu: bool, mode: int = 0, t: int = -1,
                 bufs: dict | None = None, plan: bool = True, ws: torch.Tensor | None = None):
     """The three calls of one layer; returns device tensors and the transcript
@@ -499,6 +516,7 @@ def _outputs(n, k, device, bufs):
     return o
 
 
+@_spends_plan
 def _product_layer(ctx: Context, o: _Outputs, first, s, relu, mode, t, plan, ws):
     """A layer's three calls, first(pC, ws) its product call, which returns a
     function that gives its part of the transcript.  With t given the witness
@@ -564,6 +582,7 @@ def _product_output(n, k, C, device):
     return C, _dptr(C)
 
 
+@_spends_plan
 def ra_gate_prove(ctx: Context, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor | None = None,
                   ws: torch.Tensor | None = None):
     """The gated product's call (ra_gate_prove), in the matrix call's place:
@@ -606,6 +625,7 @@ def _embed_call(ctx: Context, tokens, E, scale, pC, pw, nw):
     return lambda: dict(c0=pr.c0, mm_evals=ev[:3 * lv], a_star=pr.a_star, b_star=pr.b_star)
 
 
+@_spends_plan
 def ra_embed_prove(ctx: Context, tokens: torch.Tensor, E: torch.Tensor, scale: int, C: torch.Tensor | None = None,
                    ws: torch.Tensor | None = None):
     """The token embedding's call (ra_embed_prove), in the matrix call's place:

@@ -503,3 +503,42 @@ def test_gated_block_without_t_equals_its_calls(ra, down):
         for x, y in zip(got, want):
             assert x["transcript"] == y["transcript"] and x["transcript"]["rs_evals"]
             assert all(torch.equal(x[key], y[key]) for key in ("C", "R", "Rm", "Y", "Z", "bits"))
+
+
+def test_an_announcement_does_not_outlive_a_refusal(ra):
+    """A layer given up before its product call, by a check in Python, by a
+    refused matrix call or by hand, leaves nothing to the next layer: the kept
+    outputs stay as they are, and the next layer, whose witness is not
+    announced, is the oracle's."""
+    rng = np.random.default_rng(33)
+    A, B = (ints(rng, (64, 64), np.int16, 300) for _ in range(2))
+    dA, dB = dev(A), dev(B)
+    E, I = dev(ints(rng, (50, 64), np.int16, 300)), dev(ints(rng, (64, 64), np.int32, 300))  # noqa: E741
+    chal = inputs.xorshift64_stream(103, 1000)
+    want = orc.prove_layer(A, B, 8, True, 0, chal, 0)
+    t = want["t"]
+    small = torch.empty(256, dtype=torch.uint8, device="cuda")
+    for how in ("tokens", "shape", "matrix", "workspace", "withdrawn"):
+        ctx, bufs = ra.Context(chal), {"C": torch.empty((64, 64), dtype=torch.int64, device="cuda")}
+        bufs["wit"] = outs = ra.witness_outputs(64, 64, "cuda")
+        for o in outs:
+            o.fill_(77)
+        if how == "withdrawn":
+            ra.ra_witness_plan(ctx, 8, True, 0, t, outs)
+            L = ra.lib()
+            one = ctypes.c_void_p(outs[0].data_ptr())
+            assert L.ra_witness_plan(ctx.h, 8, 1, 0, t, one, None, None, None, None, 4096) == -1  # some null: refused
+            assert L.ra_witness_plan(ctx.h, 0, 0, 0, -1, None, None, None, None, None, 0) == 0
+        else:
+            with pytest.raises((AssertionError, ra.RAError)):
+                if how == "tokens":  # torch's default type
+                    ra.prove_embed(ctx, torch.zeros(64, dtype=torch.int64).cuda(), E, 3, 8, True, t=t, bufs=bufs)
+                elif how == "shape":
+                    ra.prove_gate(ctx, I, I[:32], 8, True, t=t, bufs=bufs)
+                elif how == "matrix":
+                    ra.prove_layer(ctx, dA, dB[:32], 8, True, t=t, bufs=bufs)
+                else:
+                    ra.prove_layer(ctx, dA, dB, 8, True, t=t, bufs=bufs, ws=small)
+        assert ctx.cursor() == 0
+        same(ra.prove_layer(ctx, dA, dB, 8, True, t=t, plan=False), want, EMBED)
+        assert all(bool((o == 77).all()) for o in outs), how

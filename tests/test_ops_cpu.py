@@ -7,6 +7,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 from helpers import pack_planes
 from oracle import oracle as orc
@@ -212,3 +213,53 @@ def test_workspace_sizes_and_null_arguments(ra):
     assert L.ra_verify_ops(P61, 1, 1, None, None, None, None, ctypes.byref(v), ctypes.byref(f)) == -1
     assert L.ra_verify_ops(P61, 0, 0, None, None, None, None, ctypes.byref(v), ctypes.byref(f)) == -5
     assert L.ra_verify_ops(97, 1, 0, None, None, None, None, ctypes.byref(v), ctypes.byref(f)) == -2
+
+
+class Calls:
+    """Stands in for the library: every entry point is logged and succeeds.
+    `announced` says whether a witness announcement is open, as ra.h has it."""
+
+    def __init__(self):
+        self.log, self.announced = [], False
+
+    def __getattr__(self, name):
+        def call(h, *args):
+            self.log.append(name)
+            if name == "ra_witness_plan":
+                self.announced = args[4] is not None
+            return 0
+        return call
+
+
+@pytest.mark.parametrize("call", ["tokens", "shape", "type", "matrix", "raw matrix", "raw gate", "raw embed"])
+def test_a_call_refused_in_python_leaves_no_witness_announced(ra, monkeypatch, call):
+    """The layer's outputs may be freed after the refusal, so nothing may be
+    left that would have a later layer's product write to them."""
+    calls = Calls()
+    monkeypatch.setattr(ra, "lib", lambda: calls)
+    monkeypatch.setattr(ra, "_dptr", lambda t: ctypes.c_void_p(t.data_ptr()))
+    ctx = ra.Context.__new__(ra.Context)
+    ctx.h, ctx.deferred, ctx._fills = ctypes.c_void_p(8), False, []
+    I = torch.zeros((4, 8), dtype=torch.int32)  # noqa: E741
+    S, tok = torch.zeros((4, 8), dtype=torch.int16), torch.zeros(4, dtype=torch.int64)
+    bufs = {}
+    refused = {"tokens": lambda: ra.prove_embed(ctx, tok, S, 3, 4, t=5, bufs=bufs),
+               "shape": lambda: ra.prove_gate(ctx, I, I[:2], 4, t=5, bufs=bufs),
+               "type": lambda: ra.prove_gate(ctx, I.double(), I, 4, t=5, bufs=bufs),
+               "matrix": lambda: ra.prove_layer(ctx, I, I.T.contiguous(), 4, True, t=5, bufs=bufs),
+               "raw matrix": lambda: ra.ra_sumcheck_matmul_prove(ctx, I, I.T.contiguous()),
+               "raw gate": lambda: ra.ra_gate_prove(ctx, I, I, C=I),
+               "raw embed": lambda: ra.ra_embed_prove(ctx, tok, S, 3)}[call]
+    if call.startswith("raw"):
+        ra.ra_witness_plan(ctx, 4, True, 0, 5, ra.witness_outputs(4, 4, "cpu"))
+        assert calls.announced
+    with pytest.raises((AssertionError, KeyError)):
+        refused()
+    assert "ra_witness_plan" in calls.log and not calls.announced, calls.log
+    assert not any(name.endswith("_prove") for name in calls.log)
+    ctx.h = None
+
+
+def test_an_announcement_is_withdrawn_by_null_buffers_only(ra):
+    L = ra.lib()
+    assert L.ra_witness_plan(None, 0, 0, 0, -1, None, None, None, None, None, 0) == -1
