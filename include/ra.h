@@ -385,8 +385,12 @@ ra_status ra_gate_workspace_size(uint32_t n, uint32_t k, size_t *bytes);
  * the verifier computes it from the tokens), b_star = E~(rho, r2).  Challenges:
  * r1 (log n), r2 (log k), rho (log V).
  *   d_tokens  n int32 in [-1, vocab); any other value is not followed (a row
- *             of zeros) and makes the call's status RA_E_INVAL (a synchronous
- *             call then consumes nothing).
+ *             of zeros) and makes the call's status RA_E_INVAL.  Found by this
+ *             call's own wait, or in deferred mode by any wait before the
+ *             layer's range call is enqueued, the layer is given up: its
+ *             challenges are given back and the context is between layers
+ *             (its further calls are RA_E_STATE).  Found later, the layer
+ *             stands as enqueued and the next wait reports it.
  *   d_E       vocab x d int16, rows lde >= d entries apart.
  *   scale     fixed-point factor, any int32.
  *   d_C       out, n x k int64, k = d rounded up to a power of two (columns

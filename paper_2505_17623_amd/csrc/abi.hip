@@ -45,7 +45,6 @@ struct ra_ctx {
     bool link_ok = false;  // a layer over F_p has just been proven: its a* may be linked (ra_link_prove)
     const int64_t *mm_of = nullptr;  // the product whose partial minima and maxima are in d_wit
     int mm_parts = 0;
-    uint64_t refused = 0;   // challenges that a refused embedding has to give back
     bool is_matrix = true;  // the layer's product is a matrix product: its a* is a claim on its input
     sha::Transcript *d_fs = nullptr;  // the Fiat-Shamir transcript (ra_ctx_create_fs), on the device
     size_t eq_cap = 0;
@@ -327,16 +326,26 @@ ra_status finish(ra_ctx *c, size_t off, std::function<ra_status(const uint64_t *
     return d;
 }
 
-// A refused embedding found at a wait of its own layer gives its challenges
-// back and leaves the context between layers, its announced witness dropped.
-void take_back(ra_ctx *c)
+// A refused embedding, whose challenges begin at `off`, found at a wait of its
+// own layer (its range call is not enqueued yet): it gives its challenges back
+// and leaves the context between layers, its announced witness dropped.  Found
+// later, it leaves the context as it is: the layers after it are enqueued.
+void give_back(ra_ctx *c, uint64_t off)
 {
-    if (!c->refused) return;
-    c->cursor -= c->refused;
-    c->refused = 0;
+    if (c->phase == 0 || c->is_matrix || c->r12_off != off) return;
+    c->cursor = off;
     c->phase = 0;
     c->mm_of = nullptr;
     c->plan.valid = c->plan.fused = false;
+}
+
+// The status of a witness or range call that finds its layer given back by a
+// wait of its own.
+ra_status given_back(ra_ctx *c)
+{
+    const ra_status r = c->deferred_err;
+    c->deferred_err = RA_OK;
+    return r;
 }
 
 // A product call that is refused leaves the context between layers, and spends
@@ -685,7 +694,6 @@ ra_status ra_ctx_set_deferred(ra_ctx *c, int on)
     if (!on && c->deferred) {
         const ra_status r = drain(c);
         if (r != RA_OK && c->deferred_err == RA_OK) c->deferred_err = r;
-        c->refused = 0;
     }
     c->deferred = on != 0;
     return RA_OK;
@@ -697,7 +705,6 @@ ra_status ra_ctx_sync(ra_ctx *c)
     const ra_status r = drain(c);
     ra_status first = c->deferred_err != RA_OK ? c->deferred_err : r;
     c->deferred_err = RA_OK;
-    c->refused = 0;  // the layers after a refused one are enqueued already
     return first;
 }
 
@@ -935,6 +942,7 @@ ra_status ra_rescale_relu_witness(ra_ctx *c, const int64_t *d_C, uint32_t n, uin
     const int lk = log2u(k);
     size_t o_st = 0;
     if ((st = stage_take(c, 12, &o_st)) != RA_OK) return st;
+    if (c->phase != 1) return given_back(c);
     // the product's epilogue made the outputs and per-tile partials if this
     // call is the one announced; the plan is spent either way
     const auto pl = c->plan;
@@ -980,7 +988,7 @@ ra_status ra_rescale_relu_witness(ra_ctx *c, const int64_t *d_C, uint32_t n, uin
         io->rm_claim = h[9];
         io->y_claim = h[10];
         io->z_claim = h[11];
-        if (!known && !c->refused) {  // the layer state advances once t and P are known
+        if (!known && c->phase == 1) {  // the layer state advances once t and P are known
             c->s = (int)io->s;
             c->relu = (int)io->relu;
             c->mode = (int)io->round_mode;
@@ -1004,7 +1012,6 @@ ra_status ra_rescale_relu_witness(ra_ctx *c, const int64_t *d_C, uint32_t n, uin
     c->deferred = false;  // this call must wait for t and P
     st = finish(c, o_st, fill);
     c->deferred = was;
-    take_back(c);
     return st;
 }
 
@@ -1024,6 +1031,7 @@ ra_status ra_range_prove(ra_ctx *c, const uint64_t *d_bits, const int32_t *d_R, 
     if (N > kRangeMaxN) return RA_E_NOT_IMPLEMENTED;  // exact int32 sums of the plane rounds
     const uint64_t need = 4 + (uint64_t)lP + R + (relu ? lN : 0);
     ra_status st = ensure_chal(c, need);
+    if (c->phase != 2) return given_back(c);
     if (st != RA_OK) return st;
     const uint64_t *lam = c->d_chal + c->cursor, *sigma = lam + 4 + lP, *rho2 = sigma + R;
     const uint64_t *d_r12 = c->d_chal + c->r12_off;
@@ -1045,6 +1053,7 @@ ra_status ra_range_prove(ra_ctx *c, const uint64_t *d_bits, const int32_t *d_R, 
     uint64_t *WSh = (uint64_t *)(ws + rl.o_wsh);
     size_t o_tr = 0;
     if ((st = stage_take(c, trw, &o_tr)) != RA_OK) return st;
+    if (c->phase != 2) return given_back(c);
     uint64_t *part = (uint64_t *)(ws + rl.o_part), *tr = c->d_stage + o_tr;
     uint64_t *gpart = (uint64_t *)(ws + rl.o_gp), *gsum = (uint64_t *)(ws + rl.o_gs);
     const uint64_t *sigx = sigma + lP, *rz = relu ? rho2 : nullptr;
@@ -1775,7 +1784,6 @@ void begin_layer(ra_ctx *c, uint32_t n, uint32_t k, uint64_t need, const Entries
     c->phase = 1;
     c->link_ok = false;
     c->is_matrix = false;
-    c->refused = 0;
     c->plan.fused = e.wit != 0;
     c->plan.ntiles = (uint32_t)e.total;
     c->mm_of = e.wit ? nullptr : e.C;
@@ -1920,9 +1928,9 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
     }
     begin_layer(c, n, k, need, en);
     const uint64_t off = c->r12_off;
-    const ra_status r = finish(c, o_tr, [c, out, lv, need, off](const uint64_t *h) {
+    return finish(c, o_tr, [c, out, lv, off](const uint64_t *h) {
         if (h[3 + 3 * lv]) {  // a token outside [-1, vocab)
-            if (c->phase == 1 && c->r12_off == off) c->refused = need;  // found within its own layer
+            give_back(c, off);
             return (ra_status)RA_E_INVAL;
         }
         out->log_m = (uint32_t)lv;
@@ -1932,8 +1940,6 @@ extern "C" ra_status ra_embed_prove(ra_ctx *c, const int32_t *d_tokens, uint32_t
         out->b_star = h[2 + 3 * lv];
         return (ra_status)RA_OK;
     });
-    take_back(c);
-    return r;
 }
 
 // ---------------------------------------------------------------------------

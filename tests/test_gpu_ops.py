@@ -542,3 +542,122 @@ def test_an_announcement_does_not_outlive_a_refusal(ra):
         assert ctx.cursor() == 0
         same(ra.prove_layer(ctx, dA, dB, 8, True, t=t, plan=False), want, EMBED)
         assert all(bool((o == 77).all()) for o in outs), how
+
+
+def bad_embedding(ra, ctx, vocab=10):
+    """An embedding with a token outside the vocabulary, its product call alone."""
+    return ra.ra_embed_prove(ctx, dev(np.array([0, vocab], dtype=np.int32)), dev(np.ones((vocab, 8), dtype=np.int16)), 3)
+
+
+def go_on(ra, ctx, chal, start, seed=41):
+    """The context is between layers at `start`: a matrix layer with t found, a gated one and an
+    embedding with t given are the oracle's, one after the other."""
+    rng = np.random.default_rng(seed)
+    A, B, G = ints(rng, (8, 16), np.int16, 300), ints(rng, (16, 8), np.int16, 300), ints(rng, (8, 8), np.int32, 300)
+    tok, E = rng.integers(0, 9, 4).astype(np.int32), ints(rng, (9, 8), np.int16, 300)
+    assert ctx.cursor() == start
+    want = [orc.prove_layer(A, B, 8, True, 0, chal, start)]
+    want.append(orc.prove_gate_layer(G, G, 8, True, 0, chal, want[0]["cursor"], 12))
+    want.append(orc.prove_embed_layer(tok, E, 3, 4, False, 0, chal, want[1]["cursor"], 12))
+    got = [ra.prove_layer(ctx, dev(A), dev(B), 8, True), ra.prove_gate(ctx, dev(G), dev(G), 8, True, t=12),
+           ra.prove_embed(ctx, dev(tok), dev(E), 3, 4, t=12)]
+    ctx.sync()
+    for g, w, keys in zip(got, want, (EMBED, GATE, EMBED)):
+        same(g, w, keys)
+    assert ctx.cursor() == want[-1]["cursor"]
+
+
+@pytest.mark.parametrize("wait", ["sync", "synchronous", "binding", "profiling", "witness", "commitment"])
+def test_bad_token_found_by_its_own_layers_wait(ra, wait):
+    """Whatever waits between a deferred embedding's product call and its
+    witness call finds the refusal: the challenges are given back, the layer's
+    further calls are out of order, and later layers are the oracle's (no
+    challenge is given back twice)."""
+    chal = inputs.xorshift64_stream(107, 1000)
+    ctx = ra.Context(chal, deferred=True)
+    C, _ = bad_embedding(ra, ctx)
+    assert ctx.cursor() == 8  # log n, log k, log V: 1 + 3 + 4
+    code = None
+    if wait == "sync":
+        with pytest.raises(ra.RAError) as e:
+            ctx.sync()
+        code = e.value.code
+    elif wait == "synchronous":
+        ctx.set_deferred(False)
+        ctx.set_deferred(True)
+    elif wait == "binding":
+        ra.ra_mle_bind(ctx, dev(np.ones((2, 2), dtype=np.int16)), True, [5])
+    elif wait == "profiling":
+        ctx.set_profiling(False)
+    elif wait == "commitment":
+        ra.commit_generators(ctx, bytes(32), 4)
+    else:  # t found: the witness call waits
+        with pytest.raises(ra.RAError) as e:
+            ra.ra_rescale_relu_witness(ctx, C, 4, False)
+        code = e.value.code
+    assert ctx.cursor() == 0
+    with pytest.raises(ra.RAError) as e:
+        ra.ra_rescale_relu_witness(ctx, C, 4, False, t=10)
+    assert e.value.code == -7
+    if code is None:  # kept for the next sync, reported once
+        with pytest.raises(ra.RAError) as e:
+            ctx.sync()
+        code = e.value.code
+    assert code == -1
+    ctx.sync()
+    go_on(ra, ctx, chal, 0)
+
+
+def test_bad_token_found_between_witness_and_range(ra):
+    """The layer's range call is not enqueued yet: given back as well; enqueued, the layer stands."""
+    chal = inputs.xorshift64_stream(109, 1000)
+    for enqueued in (False, True):
+        ctx = ra.Context(chal, deferred=True)
+        C, _ = bad_embedding(ra, ctx)
+        (R, _, Y, _, bits), info = ra.ra_rescale_relu_witness(ctx, C, 4, False, t=10)
+        if enqueued:
+            ra.ra_range_prove(ctx, bits, R, Y, info)
+        start = ctx.cursor() if enqueued else 0
+        with pytest.raises(ra.RAError) as e:
+            ctx.sync()
+        assert e.value.code == -1 and ctx.cursor() == start
+        if not enqueued:
+            with pytest.raises(ra.RAError) as e:
+                ra.ra_range_prove(ctx, bits, R, Y, info)
+            assert e.value.code == -7
+        go_on(ra, ctx, chal, start)
+
+
+def test_bad_token_found_when_the_pinned_area_grows(ra):
+    """With the area (4096 words at first) all but full of pending outputs, a call of the
+    refused layer itself waits for it to grow.  Whichever call that is, the
+    layer is given back or stands, and the context goes on from its cursor."""
+    chal = inputs.xorshift64_stream(113, 20000)
+    rng = np.random.default_rng(43)
+    G = dev(ints(rng, (1, 1), np.int32, 100))
+    found = set()
+    # a gated layer of one entry leaves 8 + 16 + 24 words pending (s + t + 2 = 16 planes: 4 rounds of 4 words and
+    # six, rounded up to eights), 84 of them 4032; the embedding's product takes 4 + 3 log V, rounded up: 8 .. 56,
+    # its witness 16 and its range call 56
+    for lv in (1, 4, 6, 9, 12, 14, 17):
+        ctx = ra.Context(chal, deferred=True)
+        for _ in range(84):
+            ra.prove_gate(ctx, G, G, 8, t=6)
+        start, where = ctx.cursor(), "later"
+        C, _ = bad_embedding(ra, ctx, 1 << lv)
+        try:
+            (R, _, Y, _, bits), info = ra.ra_rescale_relu_witness(ctx, C, 4, False, t=10)
+            where = "range"
+            ra.ra_range_prove(ctx, bits, R, Y, info)
+            start, where = ctx.cursor(), "stands"
+        except ra.RAError as e:
+            assert e.code == -1 and ctx.cursor() == start
+            where = "witness" if where == "later" else where
+            ctx.sync()
+        else:
+            with pytest.raises(ra.RAError) as e:
+                ctx.sync()
+            assert e.value.code == -1
+        found.add(where)
+        go_on(ra, ctx, chal, start)
+    assert {"witness", "range"} <= found, found
