@@ -783,6 +783,36 @@ def unpack_bits(words: np.ndarray, P: int) -> np.ndarray:
     return ((w[None, :] >> q) & np.uint64(1)).astype(np.uint8)
 
 
+def _host_ints(x, dtype, what):
+    """x as a contiguous array of `dtype`; ValueError where a value would not be the same."""
+    a = np.asarray(x)
+    if a.dtype != dtype:
+        if a.size and a.dtype.kind not in "iu":
+            raise ValueError(f"{what}: integers wanted, not {a.dtype}")
+        info = np.iinfo(dtype)
+        if a.size and (int(a.min()) < info.min or int(a.max()) > info.max):
+            raise ValueError(f"{what}: values past {np.dtype(dtype)}")
+        a = a.astype(dtype)
+    return np.ascontiguousarray(a)
+
+
+def _int_matrix(x, what):
+    """x as a contiguous int16 or int32 matrix: kept in either type, else converted to int32."""
+    a = _host_ints(x, np.int16 if np.asarray(x).dtype == np.int16 else np.int32, what)
+    if a.ndim != 2:
+        raise ValueError(f"{what}: a matrix wanted, not {a.ndim} dimensions")
+    return a
+
+
+def _gate_factors(A, B):
+    """The two factors of a gated product, one row repeated for all where it is given alone."""
+    A, B = _int_matrix(A, "A"), _int_matrix(B, "B")
+    n = max(A.shape[0], B.shape[0])
+    if A.shape[1] != B.shape[1] or any(x.shape[0] not in (1, n) for x in (A, B)):
+        raise ValueError(f"factors of {A.shape} and {B.shape} entries")
+    return [np.ascontiguousarray(np.broadcast_to(x, (n, x.shape[1]))) for x in (A, B)]
+
+
 def ra_verify(challenges, layers):
     """Host verifier.  `challenges` is a seed (int: ra_verify draws the
     stream) or an array of challenges (ra_verify_stream).  `layers` is a
@@ -790,8 +820,9 @@ def ra_verify(challenges, layers):
     and the transcript dict; returns (verdict, failed_layer).
 
     Layers of another product (with a seed only: ra_verify_ops) are told by
-    their dicts: a gated product has "B" an int16 or int32 n x k factor and a
-    transcript with gate_evals; an embedding has "tokens", "scale" and "B" the
+    their dicts: a gated product has "A" and "B" its n x k factors (integers
+    within int32; one row stands for n of the same) and a transcript with
+    gate_evals; an embedding has "tokens", "scale" and "B" the
     table.  "from_a" / "from_b" (any layer / a gated product): the index of the
     earlier layer whose Z that input must equal."""
     seeded = isinstance(challenges, (int, np.integer))
@@ -810,8 +841,11 @@ def ra_verify(challenges, layers):
         op = ops[i]
         op.from_a, op.from_b = L.get("from_a", -1), L.get("from_b", -1)
         special |= gate or embed or op.from_a >= 0 or op.from_b >= 0
-        B = np.ascontiguousarray(L["B"], dtype=None if gate else np.int16)
-        A = np.zeros((1, 1), dtype=np.int16) if embed else np.ascontiguousarray(L["A"])
+        if gate:
+            A, B = _gate_factors(L["A"], L["B"])
+        else:
+            B = np.ascontiguousarray(L["B"], dtype=np.int16)
+            A = np.zeros((1, 1), dtype=np.int16) if embed else np.ascontiguousarray(L["A"])
         n, m = A.shape
         k = B.shape[1]
         if gate:

@@ -263,3 +263,44 @@ def test_a_call_refused_in_python_leaves_no_witness_announced(ra, monkeypatch, c
 def test_an_announcement_is_withdrawn_by_null_buffers_only(ra):
     L = ra.lib()
     assert L.ra_witness_plan(None, 0, 0, 0, -1, None, None, None, None, None, 0) == -1
+
+
+def gated_layer(A, B, seed=17):
+    """One gated layer, proven by the oracle, as ra_verify takes it."""
+    A, B = np.broadcast_arrays(np.asarray(A, dtype=np.int64), np.asarray(B, dtype=np.int64))
+    return seed, abi(orc.prove_gate_layer(A.copy(), B.copy(), 8, False, 0, inputs.xorshift64_stream(seed, 400), 0))
+
+
+@pytest.mark.parametrize("side", ["A", "B"])
+def test_verifier_takes_one_row_of_a_gated_product_for_all(ra, side):
+    """The prover's factors may be one row for all n (a learned scale); given to
+    the verifier alone, it stands for n rows and is not read past its end."""
+    rng = np.random.default_rng(2)
+    full, row = rng.integers(-900, 900, (8, 4)).astype(np.int32), rng.integers(-900, 900, (1, 4)).astype(np.int16)
+    seed, layer = gated_layer(*((row, full) if side == "A" else (full, row)))
+    other = "B" if side == "A" else "A"
+    assert ra.ra_verify(seed, [dict(layer, **{side: row, other: full})]) == (0, 0)
+    bad = row.copy()
+    bad[0, 3] += 1
+    assert ra.ra_verify(seed, [dict(layer, **{side: bad, other: full})]) == (3, 0)
+
+
+@pytest.mark.parametrize("dtype", [np.int8, np.uint16, np.int16, np.int32, np.int64, np.uint64])
+def test_verifier_takes_a_gated_products_factors_in_any_integer_type(ra, dtype):
+    rng = np.random.default_rng(4)
+    A, B = rng.integers(0, 100, (2, 4, 8))
+    seed, layer = gated_layer(A, B)
+    for x, y in ((A.astype(dtype), B.astype(np.int32)), (A.astype(np.int32), B.astype(dtype)), (A.astype(dtype), B.astype(dtype))):
+        assert ra.ra_verify(seed, [dict(layer, A=x, B=y)]) == (0, 0)
+
+
+def test_verifier_refuses_other_factors_of_a_gated_product(ra):
+    rng = np.random.default_rng(6)
+    A, B = rng.integers(-100, 100, (2, 4, 8)).astype(np.int32)
+    seed, layer = gated_layer(A, B)
+    past = A.astype(np.int64)
+    past[1, 2] = 2 ** 31
+    for x, y in ((A[:, :4], B), (A, B[:, :4]), (A[:2], B), (A, B[:3]), (A.reshape(-1), B), (A, B[None]), (A, past), (past, B),
+                 (A.astype(np.float16), B), (A, B.astype(np.float64)), (A, B.astype(bool))):
+        with pytest.raises(ValueError):
+            ra.ra_verify(seed, [dict(layer, A=x, B=y)])
