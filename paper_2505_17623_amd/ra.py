@@ -796,9 +796,9 @@ def _host_ints(x, dtype, what):
     return np.ascontiguousarray(a)
 
 
-def _int_matrix(x, what):
-    """x as a contiguous int16 or int32 matrix: kept in either type, else converted to int32."""
-    a = _host_ints(x, np.int16 if np.asarray(x).dtype == np.int16 else np.int32, what)
+def _int_matrix(x, what, dtype=None):
+    """x as a contiguous matrix of `dtype` (None: int16 or int32, kept in either, else converted to int32)."""
+    a = _host_ints(x, dtype or (np.int16 if np.asarray(x).dtype == np.int16 else np.int32), what)
     if a.ndim != 2:
         raise ValueError(f"{what}: a matrix wanted, not {a.ndim} dimensions")
     return a
@@ -813,11 +813,33 @@ def _gate_factors(A, B):
     return [np.ascontiguousarray(np.broadcast_to(x, (n, x.shape[1]))) for x in (A, B)]
 
 
+def _matrix_factors(A, B):
+    A, B = _int_matrix(A, "A"), _int_matrix(B, "B", np.int16)
+    if A.shape[1] != B.shape[0]:
+        raise ValueError(f"factors of {A.shape} and {B.shape} entries")
+    return A, B
+
+
+def _layer_tables(L, N):
+    """A layer's tables as the verifier reads them, N entries each (Rm and bits
+    also as the signed type that holds their bits on the device)."""
+    arrs = {key: _host_ints(L[key], np.int32, key) for key in ("Z", "R", "Y")}
+    for key, signed, dtype in (("Rm", np.int16, np.uint16), ("bits", np.int64, np.uint64)):
+        a = np.asarray(L[key])
+        arrs[key] = np.ascontiguousarray(a).view(dtype) if a.dtype == signed else _host_ints(a, dtype, key)
+    for key, a in arrs.items():
+        if a.size != N:
+            raise ValueError(f"{key}: {N} entries wanted, not {a.size}")
+    return arrs
+
+
 def ra_verify(challenges, layers):
     """Host verifier.  `challenges` is a seed (int: ra_verify draws the
     stream) or an array of challenges (ra_verify_stream).  `layers` is a
     list of dicts with numpy arrays A, B, Z, R, Rm, Y, bits (uint64 words)
-    and the transcript dict; returns (verdict, failed_layer).
+    and the transcript dict; returns (verdict, failed_layer).  Integers of
+    other types are converted; ValueError where one would not stay the same or
+    an array has not the layer's size.
 
     Layers of another product (with a seed only: ra_verify_ops) are told by
     their dicts: a gated product has "A" and "B" its n x k factors (integers
@@ -844,8 +866,8 @@ def ra_verify(challenges, layers):
         if gate:
             A, B = _gate_factors(L["A"], L["B"])
         else:
-            B = np.ascontiguousarray(L["B"], dtype=np.int16)
-            A = np.zeros((1, 1), dtype=np.int16) if embed else np.ascontiguousarray(L["A"])
+            A, B = (np.zeros((1, 1), np.int16), _int_matrix(L["B"], "B", np.int16)) if embed else \
+                _matrix_factors(L["A"], L["B"])
         n, m = A.shape
         k = B.shape[1]
         if gate:
@@ -857,23 +879,21 @@ def ra_verify(challenges, layers):
             m = 0
             tr = dict(tr, a_star=0, b_star=0, mm_evals=[])
         elif embed:
-            tok = np.ascontiguousarray(L["tokens"], dtype=np.int32)
+            tok = _host_ints(L["tokens"], np.int32, "tokens")
             op.kind, op.tokens, op.scale = RA_LAYER_EMBED, tok.ctypes.data, int(L["scale"])
             op.vocab, op.d = B.shape
             keep.append(tok)
             n, m, k = tok.size, 0, 1 << (k - 1).bit_length()
-        arrs = dict(A=A, B=B, Z=np.ascontiguousarray(L["Z"], dtype=np.int32),
-                    R=np.ascontiguousarray(L["R"], dtype=np.int32),
-                    Rm=np.ascontiguousarray(np.asarray(L["Rm"]).view(np.uint16)),
-                    Y=np.ascontiguousarray(L["Y"], dtype=np.int32),
-                    bits=np.ascontiguousarray(np.asarray(L["bits"]).view(np.uint64)))
+        arrs = dict(_layer_tables(L, n * k), A=A, B=B)
         mm = np.array(tr["mm_evals"] + [0], dtype=np.uint64)
         rs = np.array(tr["rs_evals"] + [0], dtype=np.uint64)
         zc = np.array(tr["zc_evals"] + [0], dtype=np.uint64)
         keep += list(arrs.values()) + [mm, rs, zc]
         lsrc = None
         if L.get("link_src") is not None:
-            lsrc = np.ascontiguousarray(L["link_src"], dtype=np.int32)
+            lsrc = _host_ints(L["link_src"], np.int32, "link_src")
+            if lsrc.size != n * m:
+                raise ValueError(f"link_src: {n * m} entries wanted, not {lsrc.size}")
             keep.append(lsrc)
         pubs[i] = LayerPublic(n, m, k, tr["s"], tr["relu"], tr["mode"],
                               RA_I16 if A.dtype == np.int16 else RA_I32, arrs["A"].ctypes.data,
@@ -1008,15 +1028,10 @@ def _fp2_layer_structs(layers):
     keep = []
     for i, L in enumerate(layers):
         tr = L["transcript"]
-        A = np.ascontiguousarray(L["A"])
-        B = np.ascontiguousarray(L["B"], dtype=np.int16)
+        A, B = _matrix_factors(L["A"], L["B"])
         n, m = A.shape
         k = B.shape[1]
-        arrs = dict(A=A, B=B, Z=np.ascontiguousarray(L["Z"], dtype=np.int32),
-                    R=np.ascontiguousarray(L["R"], dtype=np.int32),
-                    Rm=np.ascontiguousarray(np.asarray(L["Rm"]).view(np.uint16)),
-                    Y=np.ascontiguousarray(L["Y"], dtype=np.int32),
-                    bits=np.ascontiguousarray(np.asarray(L["bits"]).view(np.uint64)))
+        arrs = dict(_layer_tables(L, n * k), A=A, B=B)
 
         def fp2_array(ev):
             a = (Fp2 * max(len(ev), 1))()

@@ -304,3 +304,61 @@ def test_verifier_refuses_other_factors_of_a_gated_product(ra):
                  (A.astype(np.float16), B), (A, B.astype(np.float64)), (A, B.astype(bool))):
         with pytest.raises(ValueError):
             ra.ra_verify(seed, [dict(layer, A=x, B=y)])
+
+
+def refused(ra, seed, layers):
+    with pytest.raises(ValueError):
+        ra.ra_verify(seed, layers)
+
+
+@pytest.mark.parametrize("key,dtype", [("tokens", np.int32), ("B", np.int16), ("Z", np.int32), ("R", np.int32),
+                                       ("Y", np.int32), ("Rm", np.uint16), ("bits", np.uint64)])
+def test_verifier_reads_an_embeddings_arrays_as_they_are(ra, key, dtype):
+    """A value that another type would not hold is not taken for the one it
+    wraps to, an array of another size is not read past its end, and other
+    integer types give the same verdict."""
+    seed, layers = network()
+    E, rest = layers[0], layers[1:]
+    whole = np.asarray(E[key])
+    wide = whole.astype(object) if key == "bits" else whole.astype(np.int64)
+    if key != "bits":  # a uint64 holds every word
+        assert ra.ra_verify(seed, [dict(E, **{key: wide}), *rest]) == (0, 0)
+        wide = wide.copy()
+        wide.flat[0] += 2 ** (8 * np.dtype(dtype).itemsize)
+        refused(ra, seed, [dict(E, **{key: wide}), *rest])
+    refused(ra, seed, [dict(E, **{key: whole.astype(np.float64)}), *rest])
+    for part in (whole[:-1], np.concatenate([whole, whole])):
+        if key == "B":  # another vocabulary is another statement, not a malformed one
+            assert ra.ra_verify(seed, [dict(E, B=part), *rest])[0] != 0
+        else:
+            refused(ra, seed, [dict(E, **{key: part}), *rest])
+    if key == "B":
+        refused(ra, seed, [dict(E, B=whole.reshape(-1)), *rest])
+
+
+def test_verifier_reads_a_matrix_layers_arrays_as_they_are(ra):
+    rng = np.random.default_rng(8)
+    A, B = rng.integers(-300, 300, (4, 8)), rng.integers(-300, 300, (8, 16))
+    layer = abi(orc.prove_layer(A, B, 8, True, 0, inputs.xorshift64_stream(23, 400), 0), A=A, B=B)
+    assert ra.ra_verify(23, [layer]) == (0, 0)  # int64 throughout
+    past = [B.copy(), A.copy()]
+    past[0][0, 0] += 1 << 16
+    past[1][0, 0] += 1 << 32
+    for bad in (dict(B=past[0]), dict(A=past[1]), dict(A=A[:, :4]), dict(B=B[:4]), dict(A=A.astype(np.float32)), dict(A=A[0]),
+                dict(Z=layer["Z"][:2]), dict(Rm=layer["Rm"].astype(np.int64) - 1 - layer["Rm"].max()), dict(bits=layer["bits"][:-1])):
+        refused(ra, 23, [dict(layer, **bad)])
+    signed = dict(layer, Rm=layer["Rm"].view(np.int16), bits=layer["bits"].view(np.int64))
+    assert ra.ra_verify(23, [signed]) == (0, 0)
+    src = np.arange(32, dtype=np.int32)
+    refused(ra, 23, [dict(layer, link_src=src[:-1])])
+
+
+def test_verifier_over_fp2_reads_a_layers_arrays_as_they_are(ra):
+    rng = np.random.default_rng(9)
+    A, B = rng.integers(-300, 300, (2, 4)), rng.integers(-300, 300, (4, 2))
+    chal = [(int(x), int(y)) for x, y in inputs.xorshift64_stream(29, 800).reshape(-1, 2)]
+    layer = abi(orc.prove_layer_fp2(A, B, 8, True, 0, chal, 0), A=A, B=B)
+    assert ra.ra_verify_fp2(29, [layer]) == (0, 0)
+    for bad in (dict(A=A[:, :2]), dict(B=B + (1 << 16)), dict(A=A.astype(np.float32)), dict(Y=layer["Y"][:1])):
+        with pytest.raises(ValueError):
+            ra.ra_verify_fp2(29, [dict(layer, **bad)])
