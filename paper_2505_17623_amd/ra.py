@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
 
 import numpy as np
@@ -612,8 +613,17 @@ def prove_gate(ctx: Context, A: torch.Tensor, B: torch.Tensor, s: int, relu: boo
     return _product_layer(ctx, o, lambda *c: _gate_call(ctx, A, B, *c), s, relu, mode, t, plan, ws)
 
 
+def _scale(scale):
+    """An embedding's factor: any int32 (ctypes would take another integer for the one it wraps to)."""
+    v = operator.index(scale)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"scale {v}: not an int32")
+    return v
+
+
 def _embed_call(ctx: Context, tokens, E, scale, pC, pw, nw):
     """The token embedding's call; returns a function for its part of the transcript."""
+    scale = _scale(scale)
     assert tokens.dtype == torch.int32 and E.dtype == torch.int16
     n, (vocab, d) = tokens.numel(), E.shape
     lv = (vocab - 1).bit_length()
@@ -880,7 +890,7 @@ def ra_verify(challenges, layers):
             tr = dict(tr, a_star=0, b_star=0, mm_evals=[])
         elif embed:
             tok = _host_ints(L["tokens"], np.int32, "tokens")
-            op.kind, op.tokens, op.scale = RA_LAYER_EMBED, tok.ctypes.data, int(L["scale"])
+            op.kind, op.tokens, op.scale = RA_LAYER_EMBED, tok.ctypes.data, _scale(L["scale"])
             op.vocab, op.d = B.shape
             keep.append(tok)
             n, m, k = tok.size, 0, 1 << (k - 1).bit_length()

@@ -362,3 +362,30 @@ def test_verifier_over_fp2_reads_a_layers_arrays_as_they_are(ra):
     for bad in (dict(A=A[:, :2]), dict(B=B + (1 << 16)), dict(A=A.astype(np.float32)), dict(Y=layer["Y"][:1])):
         with pytest.raises(ValueError):
             ra.ra_verify_fp2(29, [dict(layer, **bad)])
+
+
+@pytest.mark.parametrize("scale", [700 + 2 ** 32, 2 ** 31, -(2 ** 31) - 1])
+def test_a_scale_past_int32_is_refused(ra, monkeypatch, scale):
+    """Not taken for the int32 it wraps to, by the verifier or by the prover."""
+    seed, layers = network()
+    assert layers[0]["scale"] == 700
+    refused(ra, seed, [dict(layers[0], scale=scale), *layers[1:]])
+    monkeypatch.setattr(ra, "_dptr", lambda t: ctypes.c_void_p(t.data_ptr()))
+    calls = Calls()
+    monkeypatch.setattr(ra, "lib", lambda: calls)
+    ctx = ra.Context.__new__(ra.Context)
+    ctx.h, ctx.deferred, ctx._fills = ctypes.c_void_p(8), False, []
+    tok, E = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8), dtype=torch.int16)
+    for call in (lambda: ra.prove_embed(ctx, tok, E, scale, 4, t=5), lambda: ra.ra_embed_prove(ctx, tok, E, scale)):
+        with pytest.raises(ValueError):
+            call()
+    assert not any(name.endswith("_prove") for name in calls.log) and not calls.announced
+    ctx.h = None
+
+
+def test_a_scale_that_is_no_integer_is_refused(ra):
+    seed, layers = network()
+    for scale in (700.0, 700.5, "700"):
+        with pytest.raises(TypeError):
+            ra.ra_verify(seed, [dict(layers[0], scale=scale), *layers[1:]])
+    assert ra.ra_verify(seed, [dict(layers[0], scale=np.int64(700)), *layers[1:]]) == (0, 0)
