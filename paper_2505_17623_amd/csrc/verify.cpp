@@ -9,6 +9,7 @@
 // their multilinear extensions (Eq. (1)) at the challenge points.
 #include <algorithm>
 #include <cstring>
+#include <exception>
 #include <functional>
 #include <vector>
 
@@ -416,8 +417,10 @@ static ra_status verify_stream(uint64_t p, const uint64_t *h_challenges, uint64_
 extern "C" ra_status ra_verify_stream(uint64_t p, const uint64_t *h_challenges, uint64_t n_challenges,
                                       uint32_t n_layers, const ra_layer_public *pub, const ra_layer_tables *tables,
                                       const ra_layer_transcript *tr, int32_t *verdict, uint32_t *failed_layer)
-{
+try {
     return verify_stream(p, h_challenges, n_challenges, n_layers, pub, nullptr, tables, tr, verdict, failed_layer);
+} catch (const std::exception &) {  // a table of the layer's size does not fit in memory: no entry point throws
+    return RA_E_NOMEM;
 }
 
 // The seeded form draws as many challenges as the layers consume (their
@@ -433,7 +436,7 @@ extern "C" ra_status ra_verify(uint64_t p, uint64_t seed, uint32_t n_layers, con
 extern "C" ra_status ra_verify_ops(uint64_t p, uint64_t seed, uint32_t n_layers, const ra_layer_public *pub,
                                    const ra_layer_op *ops, const ra_layer_tables *tables,
                                    const ra_layer_transcript *tr, int32_t *verdict, uint32_t *failed_layer)
-{
+try {
     if (!verdict || !failed_layer || (n_layers && (!pub || !tables || !tr))) return RA_E_INVAL;
     if (p != kP) return RA_E_UNSUPPORTED_PRIME;
     if (seed == 0) return RA_E_SEED;
@@ -450,6 +453,8 @@ extern "C" ra_status ra_verify_ops(uint64_t p, uint64_t seed, uint32_t n_layers,
     ra::ChallengeStream cs(seed);
     for (uint64_t i = 0; i < total; i++) chal[i] = cs.next();
     return verify_stream(p, chal.data(), total, n_layers, pub, ops, tables, tr, verdict, failed_layer);
+} catch (const std::exception &) {  // a table of the layer's size does not fit in memory: no entry point throws
+    return RA_E_NOMEM;
 }
 
 // ---------------------------------------------------------------------------
@@ -658,7 +663,7 @@ int verify_layer_fp2(const ra_layer_public &L, const ra_layer_tables &T, const r
 extern "C" ra_status ra_verify_fp2(uint64_t p, uint64_t seed, uint32_t n_layers, const ra_layer_public *pub,
                                    const ra_layer_tables *tables, const ra_layer_proof_fp2 *tr, int32_t *verdict,
                                    uint32_t *failed_layer)
-{
+try {
     if (!verdict || !failed_layer || (n_layers && (!pub || !tables || !tr))) return RA_E_INVAL;
     if (p != kP) return RA_E_UNSUPPORTED_PRIME;
     if (seed == 0) return RA_E_SEED;
@@ -681,6 +686,8 @@ extern "C" ra_status ra_verify_fp2(uint64_t p, uint64_t seed, uint32_t n_layers,
         }
     }
     return RA_OK;
+} catch (const std::exception &) {  // a table of the layer's size does not fit in memory: no entry point throws
+    return RA_E_NOMEM;
 }
 
 // ---------------------------------------------------------------------------
@@ -761,7 +768,7 @@ G2 draw2(sha::Transcript &fs)
 extern "C" ra_status ra_verify_fs(uint64_t p, const uint8_t *domain, uint32_t n_layers, const ra_layer_public *pub,
                                   const ra_layer_tables *tables, const ra_layer_proof_fp2 *tr,
                                   const uint8_t *pub_digests, int32_t *verdict, uint32_t *failed_layer)
-{
+try {
     if (!verdict || !failed_layer || !domain || (n_layers && (!pub || !tables || !tr || !pub_digests)))
         return RA_E_INVAL;
     if (p != kP) return RA_E_UNSUPPORTED_PRIME;
@@ -816,6 +823,8 @@ extern "C" ra_status ra_verify_fs(uint64_t p, const uint8_t *domain, uint32_t n_
         }
     }
     return RA_OK;
+} catch (const std::exception &) {  // a table of the layer's size does not fit in memory: no entry point throws
+    return RA_E_NOMEM;
 }
 
 // ---------------------------------------------------------------------------

@@ -5,6 +5,8 @@ and rejects tampered ones.  No GPU compute call is made here."""
 import ctypes
 import os
 import re
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -381,3 +383,48 @@ def test_commitment_field_product_top_limb(ra):
     for vals in ([2, 0], [3, 0], [-5, 7], [2 ** 31 - 1, -(2 ** 31)]):
         want = ec.encode(ec.commit(vals, [P, ec.G]))
         assert ra.commit_open(np.array(vals, dtype=np.int32), limbs, want), vals
+
+
+NO_MEMORY = """
+import ctypes, os, resource, sys
+sys.path.insert(0, {root!r})
+from paper_2505_17623_amd import ra
+L, which = ra.lib(), sys.argv[1]
+lm = 30  # the other factor's table: 2^30 words and more, and no transcript word that any check before it would miss
+u64s = lambda n: (ctypes.c_uint64 * n)()
+small = (ctypes.c_int64 * 8)(-1)
+at = ctypes.addressof(small)
+gate = which == "ra_verify_ops"
+pub = ra.LayerPublic(1, 0 if gate else 1 << lm, 1, 1, 0, 1, ra.RA_I16, at, at, at, 0, None)
+tab = ra.LayerTables(at, at, at, at)
+v, f = ctypes.c_int32(-1), ctypes.c_uint32()
+tr = ra.LayerTranscript()
+tr.mm.log_m, tr.mm.evals = lm, u64s(3 * lm)
+tr.wit = ra.WitnessInfo(1, 0, 1, 0, 4, 0, 0, 0, 0)
+tr.rng.rounds, tr.rng.evals = 2, u64s(8)
+p2 = ra.LayerProofFp2(s=1, relu=0, round_mode=1, t=0, P=4, log_m=lm, rounds=2)
+p2.mm_evals, p2.rs_evals = (ra.Fp2 * (3 * lm))(), (ra.Fp2 * 8)()
+op = ra.LayerOp(kind=ra.RA_LAYER_EMBED, from_a=-1, from_b=-1, tokens=at, vocab=1 << lm, d=1, scale=1)
+chal, end = u64s(200), (ctypes.byref(v), ctypes.byref(f))
+R = lambda x: ctypes.byref(x)
+with open("/proc/self/statm") as fh:
+    used = int(fh.read().split()[0]) * os.sysconf("SC_PAGE_SIZE")
+resource.setrlimit(resource.RLIMIT_AS, (used + (1 << 29), used + (1 << 29)))
+if which == "ra_verify_ops":
+    st = L.ra_verify_ops(ra.P61, 5, 1, R(pub), R(op), R(tab), R(tr), *end)
+elif which == "ra_verify_stream":
+    st = L.ra_verify_stream(ra.P61, chal, 200, 1, R(pub), R(tab), R(tr), *end)
+elif which == "ra_verify_fp2":
+    st = L.ra_verify_fp2(ra.P61, 5, 1, R(pub), R(tab), R(p2), *end)
+else:
+    st = L.ra_verify_fs(ra.P61, bytes(32), 1, R(pub), R(tab), R(p2), bytes(32), *end)
+print("status", st, flush=True)
+"""
+
+
+@pytest.mark.parametrize("entry", ["ra_verify_ops", "ra_verify_stream", "ra_verify_fp2", "ra_verify_fs"])
+def test_a_verifier_out_of_memory_returns_a_status(ra, entry):
+    """A statement whose tables do not fit in memory (the process may take
+    another 512 MiB) is RA_E_NOMEM: no exception leaves an entry point."""
+    r = subprocess.run([sys.executable, "-c", NO_MEMORY.format(root=ROOT), entry], capture_output=True, text=True, timeout=300)
+    assert r.stdout.split() == ["status", "-11"], (r.returncode, r.stdout, r.stderr[-400:])
