@@ -397,6 +397,11 @@ def witness_outputs(n: int, k: int, device):
             torch.empty(n * k, dtype=torch.int64, device=device))    # uint64 words
 
 
+def _check_witness_outputs(outs, N):
+    for tsr, dt in zip(outs, (torch.int32, torch.int16, torch.int32, torch.int32, torch.int64)):
+        assert tsr.dtype == dt and tsr.numel() == N and tsr.is_contiguous()
+
+
 def ra_rescale_relu_witness(ctx: Context, C: torch.Tensor, s: int, relu: bool, mode: int = 0, t: int = -1,
                             outs=None, ws: torch.Tensor | None = None):
     """Returns ((R, Rm, Y, Z, bits), info).  info.t and info.P are set on return
@@ -405,8 +410,7 @@ def ra_rescale_relu_witness(ctx: Context, C: torch.Tensor, s: int, relu: bool, m
     witness_outputs."""
     n, k = C.shape
     R, Rm, Y, Z, bits = witness_outputs(n, k, C.device) if outs is None else outs
-    for tsr, dt in ((R, torch.int32), (Rm, torch.int16), (Y, torch.int32), (Z, torch.int32), (bits, torch.int64)):
-        assert tsr.dtype == dt and tsr.numel() == n * k and tsr.is_contiguous()
+    _check_witness_outputs((R, Rm, Y, Z, bits), n * k)
     info = WitnessInfo(s=s, relu=int(bool(relu)), round_mode=mode, t=t)
     _check(lib().ra_rescale_relu_witness(ctx.h, _dptr(C), n, k, _dptr(R), _dptr(Rm), _dptr(Y), _dptr(Z),
                                          _dptr(bits), n * k, *_ws(ws), ctypes.byref(info)),
@@ -418,6 +422,7 @@ def ra_witness_plan(ctx: Context, s: int, relu: bool, mode: int, t: int, outs):
     """Announce the next witness call (given t, output tensors as made by
     witness_outputs) so that the next matrix call computes it in its product."""
     R, Rm, Y, Z, bits = outs
+    _check_witness_outputs(outs, bits.numel())
     _check(lib().ra_witness_plan(ctx.h, s, int(bool(relu)), mode, t, _dptr(R), _dptr(Rm), _dptr(Y), _dptr(Z),
                                  _dptr(bits), bits.numel()), "ra_witness_plan")
 
@@ -504,7 +509,8 @@ class _Outputs:
             self.C, self.wit = bufs["C"], bufs["wit"]
         else:
             self.C, self.wit = torch.empty((n, k), dtype=torch.int64, device=device), witness_outputs(n, k, device)
-        assert self.C.shape == (n, k)
+        assert self.C.shape == (n, k) and self.C.dtype == torch.int64
+        _check_witness_outputs(self.wit, n * k)  # before the product's kernels write them
         self.ptr = [_dptr(x) for x in (self.C, *self.wit)]
         if bufs is not None:
             bufs.update(C=self.C, wit=self.wit, outputs=self)

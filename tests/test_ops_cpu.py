@@ -239,7 +239,7 @@ def test_a_call_refused_in_python_leaves_no_witness_announced(ra, monkeypatch, c
     monkeypatch.setattr(ra, "lib", lambda: calls)
     monkeypatch.setattr(ra, "_dptr", lambda t: ctypes.c_void_p(t.data_ptr()))
     ctx = ra.Context.__new__(ra.Context)
-    ctx.h, ctx.deferred, ctx._fills = ctypes.c_void_p(8), False, []
+    ctx.h, ctx.deferred, ctx._fills = None, False, []
     I = torch.zeros((4, 8), dtype=torch.int32)  # noqa: E741
     S, tok = torch.zeros((4, 8), dtype=torch.int16), torch.zeros(4, dtype=torch.int64)
     bufs = {}
@@ -257,7 +257,6 @@ def test_a_call_refused_in_python_leaves_no_witness_announced(ra, monkeypatch, c
         refused()
     assert "ra_witness_plan" in calls.log and not calls.announced, calls.log
     assert not any(name.endswith("_prove") for name in calls.log)
-    ctx.h = None
 
 
 def test_an_announcement_is_withdrawn_by_null_buffers_only(ra):
@@ -374,13 +373,12 @@ def test_a_scale_past_int32_is_refused(ra, monkeypatch, scale):
     calls = Calls()
     monkeypatch.setattr(ra, "lib", lambda: calls)
     ctx = ra.Context.__new__(ra.Context)
-    ctx.h, ctx.deferred, ctx._fills = ctypes.c_void_p(8), False, []
+    ctx.h, ctx.deferred, ctx._fills = None, False, []
     tok, E = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8), dtype=torch.int16)
     for call in (lambda: ra.prove_embed(ctx, tok, E, scale, 4, t=5), lambda: ra.ra_embed_prove(ctx, tok, E, scale)):
         with pytest.raises(ValueError):
             call()
     assert not any(name.endswith("_prove") for name in calls.log) and not calls.announced
-    ctx.h = None
 
 
 def test_a_scale_that_is_no_integer_is_refused(ra):
@@ -389,3 +387,27 @@ def test_a_scale_that_is_no_integer_is_refused(ra):
         with pytest.raises(TypeError):
             ra.ra_verify(seed, [dict(layers[0], scale=scale), *layers[1:]])
     assert ra.ra_verify(seed, [dict(layers[0], scale=np.int64(700)), *layers[1:]]) == (0, 0)
+
+
+@pytest.mark.parametrize("which", range(6))
+def test_a_callers_outputs_of_another_size_or_type_are_refused(ra, monkeypatch, which):
+    """Before anything is announced or called: the product's kernels write them."""
+    calls = Calls()
+    monkeypatch.setattr(ra, "lib", lambda: calls)
+    monkeypatch.setattr(ra, "_dptr", lambda t: ctypes.c_void_p(t.data_ptr()))
+    monkeypatch.setattr(ra, "_rows", lambda t: (ctypes.c_void_p(t.data_ptr()), t.stride(0)))
+    ctx = ra.Context.__new__(ra.Context)
+    ctx.h, ctx.deferred, ctx._fills = None, False, []
+    tok, E = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8), dtype=torch.int16)
+    I = torch.zeros((4, 8), dtype=torch.int32)  # noqa: E741
+    for change in (lambda x: x[:1], lambda x: x.to(torch.int8)):
+        outs = [torch.empty((4, 8), dtype=torch.int64), *ra.witness_outputs(4, 8, "cpu")]
+        outs[which] = change(outs[which])
+        entries = [lambda b: ra.prove_embed(ctx, tok, E, 3, 4, t=5, bufs=b), lambda b: ra.prove_gate(ctx, I, I, 4, t=5, bufs=b),
+                   lambda b: ra.prove_gate(ctx, I, I, 4, bufs=b), lambda b: ra.prove_layer(ctx, I[:, :4], E, 4, True, t=5, bufs=b)]
+        if which > 0:  # an announcement has no C
+            entries.append(lambda b: ra.ra_witness_plan(ctx, 4, True, 0, 5, b["wit"]))
+        for call in entries:
+            with pytest.raises(AssertionError):
+                call({"C": outs[0], "wit": tuple(outs[1:])})
+    assert not calls.announced and not any(name.endswith("_prove") for name in calls.log)
