@@ -247,6 +247,7 @@ class Context:
                    "ra_ctx_create_stream")
         self.h = h
         self._fills = []  # Python-side results completed at sync (deferred mode)
+        self._held = []   # the structs that the library fills then
         self.deferred = False
         if deferred:
             self.set_deferred(True)
@@ -260,8 +261,15 @@ class Context:
 
     def _run_fills(self):
         fills, self._fills = self._fills, []
+        self._held.clear()  # filled
         for f in fills:
             f()
+
+    def hold(self, *structs):
+        """Keep what a call that has been enqueued fills at the next sync, also
+        where a later call of the layer is refused and nothing else keeps it."""
+        if self.deferred:
+            self._held.append(structs)
 
     def later(self, fill):
         """Run `fill` now (synchronous mode) or at the next sync (deferred mode)."""
@@ -415,6 +423,7 @@ def ra_rescale_relu_witness(ctx: Context, C: torch.Tensor, s: int, relu: bool, m
     _check(lib().ra_rescale_relu_witness(ctx.h, _dptr(C), n, k, _dptr(R), _dptr(Rm), _dptr(Y), _dptr(Z),
                                          _dptr(bits), n * k, *_ws(ws), ctypes.byref(info)),
            "ra_rescale_relu_witness")
+    ctx.hold(info)
     return (R, Rm, Y, Z, bits), info
 
 
@@ -541,6 +550,7 @@ def _product_layer(ctx: Context, o: _Outputs, first, s, relu, mode, t, plan, ws)
         product = first(pC, pw, nw)
         _check(L.ra_rescale_relu_witness(ctx.h, pC, n, k, pR, pRm, pY, pZ, pbits, N, pw, nw, ctypes.byref(info)),
                "ra_rescale_relu_witness")
+        ctx.hold(info)
     finally:
         if join:
             ctx.set_deferred(False)
@@ -579,6 +589,7 @@ def _gate_call(ctx: Context, A, B, pC, pw, nw):
     (pa, lda), (pb, ldb) = _rows(A), _rows(B)
     _check(lib().ra_gate_prove(ctx.h, pa, _DT[A.dtype], lda, pb, _DT[B.dtype], ldb, n, k, pC, pw, nw,
                                ctypes.byref(pr)), "ra_gate_prove")
+    ctx.hold(pr, ev)
     return lambda: dict(c0=pr.c0, gate_evals=ev[:4 * lN], a_at=pr.a_at, b_at=pr.b_at)
 
 
@@ -638,6 +649,7 @@ def _embed_call(ctx: Context, tokens, E, scale, pC, pw, nw):
     pe, lde = _rows(E)
     _check(lib().ra_embed_prove(ctx.h, _dptr(tokens), n, pe, lde, vocab, d, scale, pC, pw, nw, ctypes.byref(pr)),
            "ra_embed_prove")
+    ctx.hold(pr, ev)
     return lambda: dict(c0=pr.c0, mm_evals=ev[:3 * lv], a_star=pr.a_star, b_star=pr.b_star)
 
 

@@ -4,6 +4,8 @@ pure Python, the library's verifier on the oracle's proofs and on tampered
 ones, and the calls' refusals that need no GPU."""
 import copy
 import ctypes
+import gc
+import weakref
 
 import numpy as np
 import pytest
@@ -239,7 +241,7 @@ def test_a_call_refused_in_python_leaves_no_witness_announced(ra, monkeypatch, c
     monkeypatch.setattr(ra, "lib", lambda: calls)
     monkeypatch.setattr(ra, "_dptr", lambda t: ctypes.c_void_p(t.data_ptr()))
     ctx = ra.Context.__new__(ra.Context)
-    ctx.h, ctx.deferred, ctx._fills = None, False, []
+    ctx.h, ctx.deferred, ctx._fills, ctx._held = None, False, [], []
     I = torch.zeros((4, 8), dtype=torch.int32)  # noqa: E741
     S, tok = torch.zeros((4, 8), dtype=torch.int16), torch.zeros(4, dtype=torch.int64)
     bufs = {}
@@ -373,7 +375,7 @@ def test_a_scale_past_int32_is_refused(ra, monkeypatch, scale):
     calls = Calls()
     monkeypatch.setattr(ra, "lib", lambda: calls)
     ctx = ra.Context.__new__(ra.Context)
-    ctx.h, ctx.deferred, ctx._fills = None, False, []
+    ctx.h, ctx.deferred, ctx._fills, ctx._held = None, False, [], []
     tok, E = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8), dtype=torch.int16)
     for call in (lambda: ra.prove_embed(ctx, tok, E, scale, 4, t=5), lambda: ra.ra_embed_prove(ctx, tok, E, scale)):
         with pytest.raises(ValueError):
@@ -397,7 +399,7 @@ def test_a_callers_outputs_of_another_size_or_type_are_refused(ra, monkeypatch, 
     monkeypatch.setattr(ra, "_dptr", lambda t: ctypes.c_void_p(t.data_ptr()))
     monkeypatch.setattr(ra, "_rows", lambda t: (ctypes.c_void_p(t.data_ptr()), t.stride(0)))
     ctx = ra.Context.__new__(ra.Context)
-    ctx.h, ctx.deferred, ctx._fills = None, False, []
+    ctx.h, ctx.deferred, ctx._fills, ctx._held = None, False, [], []
     tok, E = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8), dtype=torch.int16)
     I = torch.zeros((4, 8), dtype=torch.int32)  # noqa: E741
     for change in (lambda x: x[:1], lambda x: x.to(torch.int8)):
@@ -411,3 +413,44 @@ def test_a_callers_outputs_of_another_size_or_type_are_refused(ra, monkeypatch, 
             with pytest.raises(AssertionError):
                 call({"C": outs[0], "wit": tuple(outs[1:])})
     assert not calls.announced and not any(name.endswith("_prove") for name in calls.log)
+
+
+@pytest.mark.parametrize("kind", ["gate", "embed", "matrix"])
+@pytest.mark.parametrize("refusing", ["ra_rescale_relu_witness", "ra_range_prove"])
+def test_a_layer_refused_midway_keeps_what_the_library_still_fills(ra, monkeypatch, kind, refusing):
+    """Deferred: the product's and the witness's structs and arrays are written
+    at the next sync, so they stay although the layer's later call is refused."""
+    structs = {}
+
+    class Refusing(Calls):
+        def __getattr__(self, name):
+            def call(h, *args):
+                if name == refusing:
+                    return -9
+                if name == "ra_rescale_relu_witness":
+                    args[-1]._obj.P = 16  # known at once
+                if args and hasattr(args[-1], "_obj"):
+                    structs[name] = weakref.ref(args[-1]._obj)
+                return 0
+            return call
+    calls = Refusing()
+    monkeypatch.setattr(ra, "lib", lambda: calls)
+    monkeypatch.setattr(ra, "_dptr", lambda t: ctypes.c_void_p(t.data_ptr()))
+    monkeypatch.setattr(ra, "_rows", lambda t: (ctypes.c_void_p(t.data_ptr()), t.stride(0)))
+    ctx = ra.Context.__new__(ra.Context)
+    ctx.h, ctx.deferred, ctx._fills, ctx._held = None, True, [], []
+    tok, E = torch.zeros(4, dtype=torch.int32), torch.zeros((4, 8), dtype=torch.int16)
+    I = torch.zeros((4, 8), dtype=torch.int32)  # noqa: E741
+    with pytest.raises(ra.RAError):
+        if kind == "gate":
+            ra.prove_gate(ctx, I, I, 8, t=3, plan=False)
+        elif kind == "embed":
+            ra.prove_embed(ctx, tok, E, 3, 8, t=3, plan=False)
+        else:
+            ra.prove_layer(ctx, I[:, :4], E, 8, False, t=3, plan=False)
+    gc.collect()
+    want = 1 if refusing == "ra_rescale_relu_witness" else 2
+    assert len(structs) == want and all(r() is not None for r in structs.values()), structs
+    ctx.sync()
+    gc.collect()
+    assert all(r() is None for r in structs.values())
