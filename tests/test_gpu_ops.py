@@ -661,3 +661,121 @@ def test_bad_token_found_when_the_pinned_area_grows(ra):
         found.add(where)
         go_on(ra, ctx, chal, start)
     assert {"witness", "range"} <= found, found
+
+
+@pytest.mark.parametrize("n,vocab,d,ld", [(4, 16400, 70, 70), (2, 16385, 33, 35), (1, 16400, 1100, 1100), (2, 40, 1100, 1100),
+                                          (1, 40, 1101, 1101), (2, 40, 2080, 2080), (1, 100, 4127, 4130)])
+@pytest.mark.parametrize("t", [-1, 15])
+def test_embed_wide_tables_match_oracle(ra, n, vocab, d, ld, t):
+    """The table's pass past its first trip: a quarter of a row of more than
+    eight chunks of 32 entries (d > 1024), a ragged last chunk or none, rows at
+    odd strides, in both heights of a workgroup (two tiles of rows from 16384
+    padded rows on)."""
+    rng = np.random.default_rng(vocab + d)
+    wide = ints(rng, (vocab, ld), np.int16, 1 << 15)
+    wide[0, d - 1], wide[vocab - 1, d - 1] = -(1 << 15), (1 << 15) - 1
+    E = dev(wide)[:, :d]
+    tok = rng.integers(-1, vocab, n).astype(np.int32)
+    tok[0] = vocab - 1
+    chal = inputs.xorshift64_stream(300 + d, 1000)
+    want = orc.prove_embed_layer(tok, wide[:, :d], 250, 8, False, 0, chal, 0, t)
+    ctx = ra.Context(chal)
+    same(ra.prove_embed(ctx, dev(tok), E, 250, 8, t=t), want, EMBED)
+    assert ctx.cursor() == want["cursor"]
+
+
+def eq_table(z):
+    """eq(z, .) in Python integers, z's first coordinate the index's highest bit."""
+    t = [1]
+    for x in z:
+        t = [w for v in t for w in (v * (1 - x) % P61, v * x % P61)]
+    return t
+
+
+def at_point(ra, ctx, T, rows, cols):
+    """The multilinear extension of a device matrix at (rows, cols), by the two bindings."""
+    v = ra.ra_mle_bind(ctx, T, True, rows)
+    return int(ra.ra_mle_bind(ctx, v.reshape(1, -1), False, cols, field=True)[0])
+
+
+def chain_end(c0, evals, deg, rho):
+    """The last value of a sum-check whose every round's sum is the value before it."""
+    cur = c0
+    for j, x in enumerate(rho):
+        g = evals[(deg + 1) * j:(deg + 1) * (j + 1)]
+        assert (g[0] + g[1]) % P61 == cur, j
+        cur = 0
+        for a in range(deg + 1):
+            num = den = 1
+            for b in range(deg + 1):
+                if b != a:
+                    num, den = num * (x - b) % P61, den * (a - b) % P61
+            cur = (cur + g[a] * num * pow(den, P61 - 2, P61)) % P61
+    return cur
+
+
+def check_witness_of(ra, ctx, got, C, s, relu, r1, r2):
+    """The tables from C by their definitions (to nearest), the claims as the tables' extensions."""
+    R, tr = (C + (1 << (s - 1))) >> s, got["transcript"]
+    Rm, Y = C + (1 << (s - 1)) - (R << s), R.abs()
+    Z = (R + Y) // 2 if relu else R
+    assert torch.equal(got["C"], C)
+    for key, x in (("R", R), ("Y", Y), ("Z", Z)):
+        assert torch.equal(got[key].long(), x), key
+    assert torch.equal(got["Rm"].long() & 0xFFFF, Rm)
+    word = Rm + ((R + (2 << tr["t"])) << s)
+    if relu:
+        word += Y << (s + tr["t"] + 2)
+    assert torch.equal(got["bits"].reshape(C.shape), word)
+    assert tr["c0"] == at_point(ra, ctx, C, r1, r2)
+    for key, x in (("r_claim", R), ("rm_claim", Rm), ("y_claim", Y), ("z_claim", Z)):
+        assert tr[key] == at_point(ra, ctx, x.int(), r1, r2), key
+
+
+@pytest.mark.parametrize("n,vocab,d,t,off", [(8192, 999, 509, 18, 0), (8192, 999, 509, 16, 0), (65536, 50, 126, 16, 0),
+                                             (8192, 300, 251, 17, 1), (1 << 18, 7, 12, 18, 1)])
+def test_embed_of_many_rows_against_its_definition(ra, n, vocab, d, t, off):
+    """2^21 to 2^23 outputs, where a thread takes four rows at a time, once or
+    twice, in pairs of columns or (C off by one entry) alone, the claims' sums
+    reduced a row at a time (t = 18) or not."""
+    rng = np.random.default_rng(n + d)
+    k, s, scale, seed = 1 << (d - 1).bit_length(), 8, 4000, 71
+    ln, lk, lv = n.bit_length() - 1, k.bit_length() - 1, (vocab - 1).bit_length()
+    tok = rng.integers(-1, vocab, n).astype(np.int32)
+    E = dev(ints(rng, (vocab, d), np.int16, 1 << 11))
+    c = [int(x) for x in inputs.xorshift64_stream(seed, ln + lk + lv)]
+    r1, r2, rho = c[:ln], c[ln:ln + lk], c[ln + lk:]
+    ctx, help_ctx = ra.Context(seed=seed), ra.Context(seed=1)
+    buf = torch.empty(n * k + off, dtype=torch.int64, device="cuda")
+    bufs = {"C": buf[off:].reshape(n, k), "wit": ra.witness_outputs(n, k, "cuda")}
+    dt = dev(tok)
+    got = ra.prove_embed(ctx, dt, E, scale, s, t=t, bufs=bufs)
+    C = torch.zeros((n, k), dtype=torch.int64, device="cuda")
+    C[:, :d] = scale * E.long()[dt.long().clamp(min=0)] * (dt >= 0).long()[:, None]
+    check_witness_of(ra, help_ctx, got, C, s, False, r1, r2)
+    tr = got["transcript"]
+    assert chain_end(tr["c0"], tr["mm_evals"], 2, rho) == tr["a_star"] * tr["b_star"] % P61
+    e1, ev = eq_table(r1), eq_table(rho)
+    assert tr["a_star"] == scale * sum(x * ev[v] for x, v in zip(e1, tok.tolist()) if v >= 0) % P61
+    pad = torch.zeros((1 << lv, k), dtype=torch.int16, device="cuda")
+    pad[:vocab, :d] = E
+    assert tr["b_star"] == at_point(ra, help_ctx, pad, rho, r2)
+
+
+@pytest.mark.parametrize("n,k,relu", [(512, 512, True), (8192, 512, False), (2048, 4096, True)])
+def test_gate_of_many_passes_against_its_definition(ra, n, k, relu):
+    """2^18, 2^22 and 2^23 entries: two, three and four passes before the last rounds."""
+    rng = np.random.default_rng(n + k)
+    s, seed, lN, ln = 8, 73, (n * k).bit_length() - 1, n.bit_length() - 1
+    A, B = dev(ints(rng, (n, k), np.int32, 1 << 12)), dev(ints(rng, (n, k), np.int16, 1 << 11))
+    c = [int(x) for x in inputs.xorshift64_stream(seed, 2 * lN)]
+    r, rho = c[:lN], c[lN:]
+    ctx, help_ctx = ra.Context(seed=seed), ra.Context(seed=1)
+    got = ra.prove_gate(ctx, A, B, s, relu, t=15)
+    check_witness_of(ra, help_ctx, got, A.long() * B.long(), s, relu, r[:ln], r[ln:])
+    tr, eq = got["transcript"], 1
+    for x, y in zip(r, rho):
+        eq = eq * (x * y + (1 - x) * (1 - y)) % P61
+    assert chain_end(tr["c0"], tr["gate_evals"], 3, rho) == eq * tr["a_at"] * tr["b_at"] % P61
+    assert tr["a_at"] == at_point(ra, help_ctx, A, rho[:ln], rho[ln:])
+    assert tr["b_at"] == at_point(ra, help_ctx, B, rho[:ln], rho[ln:])
