@@ -1719,7 +1719,7 @@ extern "C" ra_status ra_link_prove(ra_ctx *c, const int32_t *d_Z, uint64_t z_ent
 namespace {
 struct GateLayout {
     int L, nhs;
-    size_t o_hs, o_ls, o_k, o_t0, o_t1, o_part, bytes;
+    size_t o_hs, o_ls, o_t0, o_t1, o_part, bytes;
 };
 GateLayout gate_layout(uint64_t N)
 {
@@ -1730,7 +1730,6 @@ GateLayout gate_layout(uint64_t N)
     Carve cv;
     l.o_hs = cv.take<uint64_t>(l.nhs);
     l.o_ls = cv.take<uint64_t>(2ull << l.L);
-    l.o_k = cv.take<uint64_t>(lN + 1);
     l.o_t0 = cv.take<uint64_t>(std::max<uint64_t>(N / 2, 1));
     l.o_t1 = cv.take<uint64_t>(std::max<uint64_t>(N / 2, 1));
     l.o_part = cv.take<uint64_t>((size_t)std::max(3 * lN, 1) * kEntryMaxBlocks);
@@ -1837,7 +1836,6 @@ extern "C" ra_status ra_gate_prove(ra_ctx *c, const void *d_A, ra_dtype a_dtype,
     ga.nhs = gl.nhs;
     ga.HS = (uint64_t *)(ws + gl.o_hs);
     ga.LS = (uint64_t *)(ws + gl.o_ls);
-    ga.K = (uint64_t *)(ws + gl.o_k);
     ga.T0 = (uint64_t *)(ws + gl.o_t0);
     ga.T1 = (uint64_t *)(ws + gl.o_t1);
     ga.part = (uint64_t *)(ws + gl.o_part);

@@ -530,7 +530,7 @@ struct GateArgs {
     const uint64_t *r, *rho;   // (r1, r2) and the rounds' challenges, lN each
     uint64_t *E1, *E2;         // out: the eq tables of r1 and r2
     int L, nhs;                // split of the suffix eq tables (xsetup.hpp)
-    uint64_t *HS, *LS, *K;     // nhs, 2^(L + 1) and lN + 1 words
+    uint64_t *HS, *LS;         // nhs and 2^(L + 1) words
     uint64_t *T0, *T1;         // the folded tables: 2^(lN - 1) words each at most
     uint64_t *part;            // 3 lN x kEntryMaxBlocks words
     uint64_t *tr;              // out: c0, 4 lN round words, A~(rho), B~(rho)

@@ -86,20 +86,17 @@ template <int V> struct GateProduct {
     }
 };
 
-// The suffix eq tables of r (xsetup.hpp, whose prefix products K_j the tails
-// make for themselves) by the first nx threads, the eq tables E1 (r1) and E2
-// (r2) by the others.
+// The suffix eq tables of r (xsetup.hpp; the prefix products K_j the tails make
+// for themselves) by the first nx threads, the eq tables E1 (r1) and E2 (r2) by
+// the others.
 __global__ __launch_bounds__(256) void k_gate_setup(XSetupArgs a, int nx, int ln, uint64_t *E1, uint64_t *E2)
 {
-    __shared__ uint64_t rl[64], sl[64];
-    if ((int)threadIdx.x < a.lN) {
-        rl[threadIdx.x] = a.r[threadIdx.x];
-        sl[threadIdx.x] = a.sigx[threadIdx.x];
-    }
+    __shared__ uint64_t rl[64];
+    if ((int)threadIdx.x < a.lN) rl[threadIdx.x] = a.r[threadIdx.x];
     __syncthreads();
     const uint64_t g = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (g < (uint64_t)nx) {  // nx a multiple of the workgroup
-        x_setup_body(a, (int)g, rl, sl, sl);
+    if (g < (uint64_t)nx) {
+        x_tables_body(a, (int)g, rl);
         return;
     }
     const uint64_t i = g - nx, n = 1ull << ln;
@@ -424,7 +421,7 @@ void launch_gate(const GateArgs &a, const EntriesArgs &e, hipStream_t st)
         });
         return;
     }
-    const XSetupArgs xs{a.r, a.rho, nullptr, a.lN, a.L, a.nhs, a.HS, a.LS, a.K, nullptr, nullptr, 0, 0};
+    const XSetupArgs xs{a.r, nullptr, nullptr, a.lN, a.L, a.nhs, a.HS, a.LS, nullptr, nullptr, nullptr, 0, 0};
     const int nx = (x_setup_count(xs) + kThreads - 1) / kThreads;
     const unsigned ne = (unsigned)((tables + kThreads - 1) / kThreads);
     hipLaunchKernelGGL(k_gate_setup, dim3(nx + ne), dim3(kThreads), 0, st, xs, nx * kThreads, a.lN - a.lk, a.E1, a.E2);

@@ -28,24 +28,10 @@ __host__ __device__ inline int x_setup_count(const XSetupArgs &a)
     return (a.lN > a.L ? 1 << (a.lN - a.L) : 1) + (1 << (a.L + 1)) + (a.wB > 0 ? 1 << a.wB : 0);
 }
 
-// Thread gid (0 .. x_setup_count - 1) of the set-up; rl, zl: r and the two
-// instances' challenges (sigma_x, rho'; lN words each) staged in LDS.
-__device__ __forceinline__ void x_setup_body(const XSetupArgs &a, int gid, const uint64_t *rl, const uint64_t *sl,
-                                             const uint64_t *zl)
+// Thread gid (0 .. x_setup_count - 1) of the suffix eq tables; rl: r staged in LDS.
+__device__ __forceinline__ void x_tables_body(const XSetupArgs &a, int gid, const uint64_t *rl)
 {
     const int lN = a.lN, L = a.L, nhs = a.nhs, nls = 1 << (L + 1);
-    if (gid < 128) {  // waves 0 and 1: prefix products of the two instances (lN < 64)
-        const uint64_t *z = gid < 64 ? sl : zl;
-        uint64_t *K = gid < 64 ? a.Kr : a.Kz;
-        const int j = gid & 63;
-        if (gid < 64 || a.rho2) {  // wave-uniform
-            uint64_t e = 1;
-            if (j < lN) e = m61::add(m61::mul(rl[j], z[j]), m61::mul(m61::sub(1, rl[j]), m61::sub(1, z[j])));
-            const uint64_t inc = m61::wave_prefix_mul(e);  // prod_{l <= j}
-            if (j < lN) K[j + 1] = inc;
-            if (j == 0) K[0] = 1;
-        }
-    }
     if (gid == 1) a.HS[0] = a.LS[0] = 0;  // unused heap slots
     if (gid >= 1 && gid < nhs) {
         const int s = 31 - __clz(gid);
@@ -65,6 +51,27 @@ __device__ __forceinline__ void x_setup_body(const XSetupArgs &a, int gid, const
             a.WS[w] = eq_suffix(rl, a.wj + a.wB - s, s, (uint64_t)(w - (1 << s)));
         }
     }
+}
+
+// Thread gid of the whole set-up, the tables and the prefix products; sl, zl:
+// the two instances' challenges (sigma_x, rho'; lN words each) staged in LDS.
+__device__ __forceinline__ void x_setup_body(const XSetupArgs &a, int gid, const uint64_t *rl, const uint64_t *sl,
+                                             const uint64_t *zl)
+{
+    const int lN = a.lN;
+    if (gid < 128) {  // waves 0 and 1: prefix products of the two instances (lN < 64)
+        const uint64_t *z = gid < 64 ? sl : zl;
+        uint64_t *K = gid < 64 ? a.Kr : a.Kz;
+        const int j = gid & 63;
+        if (gid < 64 || a.rho2) {  // wave-uniform
+            uint64_t e = 1;
+            if (j < lN) e = m61::add(m61::mul(rl[j], z[j]), m61::mul(m61::sub(1, rl[j]), m61::sub(1, z[j])));
+            const uint64_t inc = m61::wave_prefix_mul(e);  // prod_{l <= j}
+            if (j < lN) K[j + 1] = inc;
+            if (j == 0) K[0] = 1;
+        }
+    }
+    x_tables_body(a, gid, rl);
 }
 
 }  // namespace ra
