@@ -515,7 +515,7 @@ class _Outputs:
     def __init__(self, n, k, device, bufs=None):
         self.shape = (n, k)
         if bufs is not None and "C" in bufs:
-            self.C, self.wit = bufs["C"], bufs["wit"]
+            self.C, self.wit = bufs["C"], tuple(bufs["wit"])  # a list could change under the pointers
         else:
             self.C, self.wit = torch.empty((n, k), dtype=torch.int64, device=device), witness_outputs(n, k, device)
         assert self.C.shape == (n, k) and self.C.dtype == torch.int64

@@ -454,3 +454,17 @@ def test_a_layer_refused_midway_keeps_what_the_library_still_fills(ra, monkeypat
     ctx.sync()
     gc.collect()
     assert all(r() is None for r in structs.values())
+
+
+def test_kept_outputs_given_as_a_list_are_those_of_each_call(ra, monkeypatch):
+    """Another tensor put into the list is the one that the next call writes."""
+    monkeypatch.setattr(ra, "_dptr", lambda t: ctypes.c_void_p(t.data_ptr()))
+    wit = list(ra.witness_outputs(4, 8, "cpu"))
+    bufs = {"C": torch.empty((4, 8), dtype=torch.int64), "wit": wit}
+    for i in range(5):
+        o = ra._outputs(4, 8, "cpu", bufs)
+        assert o is ra._outputs(4, 8, "cpu", bufs)
+        assert [p.value for p in o.ptr] == [x.data_ptr() for x in (bufs["C"], *bufs["wit"])]
+        wit[i] = torch.empty_like(wit[i])
+        bufs["wit"] = wit
+    assert [p.value for p in ra._outputs(4, 8, "cpu", bufs).ptr[1:]] == [x.data_ptr() for x in wit]
