@@ -261,8 +261,8 @@ ra_status ra_rescale_relu_witness(ra_ctx *ctx, const int64_t *d_C, uint32_t n, u
  * (ra_sumcheck_matmul_prove, ra_gate_prove, ra_embed_prove) spends it, also one
  * that is refused.  All five buffers null withdraws it, for a caller that
  * gives the layer up before its product call.
- * Errors: RA_E_INVAL for a null buffer among others, t < 0 or parameters the witness call
- * would reject; RA_E_FIELD_TOO_SMALL / RA_E_NOT_IMPLEMENTED as that call
+ * Errors: RA_E_INVAL for a null buffer among others, t < 0 or parameters the
+ * witness call would reject; RA_E_FIELD_TOO_SMALL / RA_E_NOT_IMPLEMENTED as that call
  * would return them for s and t; RA_E_STATE when called between a layer's
  * calls. */
 ra_status ra_witness_plan(ra_ctx *ctx, uint32_t s, uint32_t relu, uint32_t round_mode, int32_t t, int32_t *d_R,
@@ -388,9 +388,11 @@ ra_status ra_gate_workspace_size(uint32_t n, uint32_t k, size_t *bytes);
  *             of zeros) and makes the call's status RA_E_INVAL.  Found by this
  *             call's own wait, or in deferred mode by any wait before the
  *             layer's range call is enqueued, the layer is given up: its
- *             challenges are given back and the context is between layers
- *             (its further calls are RA_E_STATE).  Found later, the layer
- *             stands as enqueued and the next wait reports it.
+ *             challenges are given back and the context is between layers.  A
+ *             witness or range call of the layer that makes that wait returns
+ *             RA_E_INVAL itself; after another call's, RA_E_STATE.  Found
+ *             later, the layer stands as enqueued and the next wait reports
+ *             it.
  *   d_E       vocab x d int16, rows lde >= d entries apart.
  *   scale     fixed-point factor, any int32.
  *   d_C       out, n x k int64, k = d rounded up to a power of two (columns

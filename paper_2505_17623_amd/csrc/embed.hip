@@ -121,12 +121,14 @@ __device__ __forceinline__ uint64_t eq_prefix_sum(const uint64_t *r2, int lk, ui
     return m61::canon(sum);
 }
 
-// A workgroup takes 16 RT rows, each of its four waves a quarter of them; U
-// chunks' loads are issued before the first is used.  Rows may start at any
-// even address; the last chunk of a width that is no multiple of 32 is read
-// entry by entry.  What bounds it is the order in which memory is asked: with
-// the waves' chunks interleaved and a chunk's rows one after the other the same
-// loads took 204 us at 128000 x 4096 (1.05 GB), so 167 (6.3 TB/s).
+// A workgroup takes 16 RT rows, each of its four waves a quarter of their
+// chunks; U chunks' loads are issued before the first is used.  Rows may start
+// at any even address; the last chunk of a width that is no multiple of 32 is
+// read entry by entry.  What bounds it is the order in which memory is asked:
+// with the waves' chunks interleaved and a chunk's rows one after the other the
+// same loads took 204 us at 128000 x 4096 (1.05 GB), so 167 (6.3 TB/s, the same
+// table again and again for one token; 185, 5.7 TB/s, where a call for 1024
+// tokens has written its outputs between).
 // The first ns workgroups scatter the tokens' weights.
 template <int RT, int U>
 __global__ __launch_bounds__(256) void k_embed_bind(EmbedArgs args, int ns, uint64_t scale)

@@ -6,7 +6,7 @@
 //
 // A thread keeps its V columns over all its rows, so a claim is sum_col E2[col]
 // (sum_row E1[row] z), E1 in limbs of 31 bits, the inner sums exact in int64 (at
-// most 2^12 rows a thread: N <= 2^31 over 2^18 threads of two columns), one
+// most 2^12 rows a thread: N <= 2^31 over 2^19 threads of a column or two), one
 // product in F_p a column at the end.  Only Rm~ and Y~ are summed: C = 2^s R +
 // Rm - half entry by entry, so R~ follows from C~, which is the sum that the
 // product's sum-check claims, and Z~ from R~ and Y~ (claims.hpp).

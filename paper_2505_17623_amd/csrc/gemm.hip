@@ -773,7 +773,7 @@ __global__ __launch_bounds__(256, 2) void k_gemm_mfma(const int8_t *__restrict__
 // quarter of the inner dimension each, straight from memory into registers (no
 // wave's fragments are another's), and their sums meet in LDS as int64.  What
 // bounds it is what one CU can read: 1 x 4096 x 1024 (int32 A, four limbs) 18
-// us against 37 with a CU's 64 steps one after the other.  Rows past n read row
+// us against 36 with a CU's 64 steps one after the other.  Rows past n read row
 // 0's limbs; their sums are not used.  Witness and tail workgroups as in
 // k_gemm_mfma.
 template <int LA, int LE>
@@ -998,10 +998,11 @@ void launch_front(const void *A, int a_is_i32, const int16_t *B, uint32_t n, uin
 }
 
 // k_gemm_rows to 32 rows and 128 workgroups, where it was never slower (launch
-// with its tail, the tiles against it, us: 1 x 64 x 64 10.0 / 8.2, 1 x 1024 x
-// 4096 14.5 / 11.6, 1 x 4096 x 1024 27 / 16 and with int32 A 33 / 18, 32 x 4096
-// x 4096 29 / 19, 1 x 32768 x 1024 155 / 73).  With one for every CU the tail,
-// which an int32 A leaves no room beside, has to wait: 1 x 64 x 8192 10 / 14.
+// with its tail and the announced witness, the tiles against it, us: 1 x 64 x
+// 64 6.4 / 5.9, 1 x 1024 x 4096 11.4 / 8.5 and with int32 A 15.7 / 8.6, 1 x 4096
+// x 1024 25 / 14 and with int32 A 36 / 18, 32 x 4096 x 4096 26 / 16, 1 x 32768 x
+// 1024 153 / 71).  With one for every CU the tail, which an int32 A leaves no
+// room beside, has to wait: 1 x 64 x 8192 7.8 / 11.8 (int16 7.0 / 5.9).
 static bool gemm_by_rows(uint32_t n, uint32_t k) { return n <= (uint32_t)kRowsMax && k <= 128u * kRowsCols; }
 
 uint32_t gemm_tiles(uint32_t n, uint32_t k)

@@ -700,8 +700,9 @@ def prove_gated_ffn(ctx: Context, X: torch.Tensor, Wg: torch.Tensor, Wu: torch.T
     t = [-1] * count if ts is None else [int(x) for x in ts]
     b = [None] * count if bufs is None else bufs
     # without ts each witness call waits for its t, and that wait completes the
-    # calls before it: one wait a layer and one at the end (64 tokens, 256 -> 683
-    # -> 256: 383 -> 352 us; one token, 1024 -> 2730 -> 1024: 398 -> 363)
+    # calls before it: one wait a layer and one at the end (kept outputs, padded
+    # dimensions: 64 tokens, 256 -> 1024 -> 256, 382 -> 353 us a block among
+    # others; one token, 1024 -> 4096 -> 1024, 396 -> 366)
     join = ts is None and not ctx.deferred
     if join:
         ctx.set_deferred(True)
