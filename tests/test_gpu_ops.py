@@ -779,3 +779,88 @@ def test_gate_of_many_passes_against_its_definition(ra, n, k, relu):
     assert chain_end(tr["c0"], tr["gate_evals"], 3, rho) == eq * tr["a_at"] * tr["b_at"] % P61
     assert tr["a_at"] == at_point(ra, help_ctx, A, rho[:ln], rho[ln:])
     assert tr["b_at"] == at_point(ra, help_ctx, B, rho[:ln], rho[ln:])
+
+
+def in_chunks(ra, ctx, T, rows, cols, log_chunk):
+    """at_point, 2^log_chunk rows at a time."""
+    hi = len(rows) - log_chunk
+    step, e = 1 << log_chunk, eq_table(rows[:hi])
+    return sum(w * at_point(ra, ctx, T[i * step:(i + 1) * step], rows[hi:], cols) for i, w in enumerate(e)) % P61
+
+
+def check_large_outputs(ra, ctx, outs, C, want, s, t, r1, r2, log_chunk):
+    """Tables and C against want(first row, last row), in chunks, and C~."""
+    R, Rm, Y, Z, bits = outs
+    step = 1 << log_chunk
+    for i in range(0, C.shape[0], step):
+        c, j = want(i, i + step), i + step
+        assert torch.equal(C[i:j], c), i
+        r = (c + (1 << (s - 1))) >> s
+        rm = c + (1 << (s - 1)) - (r << s)
+        assert torch.equal(R[i:j].long(), r) and torch.equal(Z[i:j].long(), r) and torch.equal(Y[i:j].long(), r.abs())
+        assert torch.equal(Rm[i:j].long() & 0xFFFF, rm)
+        assert torch.equal(bits.reshape(C.shape)[i:j], rm + ((r + (2 << t)) << s)), i
+    return in_chunks(ra, ctx, C, r1, r2, log_chunk)
+
+
+def test_gate_past_32_bit_offsets(ra):
+    """2^29 entries: C, the bit words and every int32 table reach past 2^31 or 2^32 bytes."""
+    n, k, s, t, seed = 1 << 15, 1 << 14, 8, 15, 77
+    lN, ln, part = 29, 15, 9
+    g = torch.Generator(device="cuda").manual_seed(1)
+    A = torch.randint(-4096, 4096, (n, k), dtype=torch.int32, device="cuda", generator=g)
+    B = torch.randint(-1024, 1024, (n, k), dtype=torch.int16, device="cuda", generator=g)
+    outs = ra.witness_outputs(n, k, "cuda")
+    ctx, help_ctx = ra.Context(seed=seed), ra.Context(seed=1)
+    ra.ra_witness_plan(ctx, s, False, 0, t, outs)
+    C, tr = ra.ra_gate_prove(ctx, A, B)
+    _, info = ra.ra_rescale_relu_witness(ctx, C, s, False, 0, t, outs)
+    c = [int(x) for x in inputs.xorshift64_stream(seed, 2 * lN)]
+    r, rho = c[:lN], c[lN:]
+    at = check_large_outputs(ra, help_ctx, outs, C, lambda i, j: A[i:j].long() * B[i:j].long(), s, t, r[:ln], r[ln:], part)
+    assert tr["c0"] == at
+    assert ((int(info.r_claim) << s) + int(info.rm_claim) - (1 << (s - 1)) - at) % P61 == 0
+    assert info.rm_claim == in_chunks(ra, help_ctx, (C + (1 << (s - 1)) & ((1 << s) - 1)).int(), r[:ln], r[ln:], part)
+    eq = 1
+    for x, y in zip(r, rho):
+        eq = eq * (x * y + (1 - x) * (1 - y)) % P61
+    assert chain_end(tr["c0"], tr["gate_evals"], 3, rho) == eq * tr["a_at"] * tr["b_at"] % P61
+    assert tr["a_at"] == in_chunks(ra, help_ctx, A, rho[:ln], rho[ln:], part)
+    assert tr["b_at"] == in_chunks(ra, help_ctx, B, rho[:ln], rho[ln:], part)
+
+
+@pytest.mark.parametrize("n,vocab,d", [(1 << 17, 300, 4096), (4, (1 << 20) + 3, 4096)])
+def test_embed_past_32_bit_offsets(ra, n, vocab, d):
+    """2^29 outputs; a table of 8.6 GB, its last rows among the tokens."""
+    s, t, scale, seed = 8, 16, 500, 79
+    ln, lk, lv = n.bit_length() - 1, 12, (vocab - 1).bit_length()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    E = torch.randint(-(1 << 15), 1 << 15, (vocab, d), dtype=torch.int16, device="cuda", generator=g)
+    tok = torch.randint(-1, vocab, (n,), dtype=torch.int32, device="cuda", generator=g)
+    tok[0], tok[n - 1] = vocab - 1, vocab - 2
+    outs = ra.witness_outputs(n, d, "cuda")
+    ctx, help_ctx = ra.Context(seed=seed), ra.Context(seed=1)
+    ra.ra_witness_plan(ctx, s, False, 0, t, outs)
+    C, tr = ra.ra_embed_prove(ctx, tok, E, scale)
+    _, info = ra.ra_rescale_relu_witness(ctx, C, s, False, 0, t, outs)
+    c = [int(x) for x in inputs.xorshift64_stream(seed, ln + lk + lv)]
+    r1, r2, rho = c[:ln], c[ln:ln + lk], c[ln + lk:]
+    part = min(ln, 11)
+
+    def want(i, j):
+        v = tok[i:j].long()
+        return scale * E[v.clamp(min=0)].long() * (v >= 0).long()[:, None]
+    at = check_large_outputs(ra, help_ctx, outs, C, want, s, t, r1, r2, part)
+    assert tr["c0"] == at
+    assert ((int(info.r_claim) << s) + int(info.rm_claim) - (1 << (s - 1)) - at) % P61 == 0
+    assert chain_end(tr["c0"], tr["mm_evals"], 2, rho) == tr["a_star"] * tr["b_star"] % P61
+    ev = eq_table(rho)
+    assert tr["a_star"] == scale * sum(x * ev[v] for x, v in zip(eq_table(r1), tok.tolist()) if v >= 0) % P61
+    v = torch.zeros(1 << lv, dtype=torch.int64, device="cuda")  # e(v), from the rows in blocks of 2^14
+    for i in range(0, vocab, 1 << 14):
+        block = E[i:i + (1 << 14)]
+        rows = 1 << (block.shape[0] - 1).bit_length()
+        if rows != block.shape[0]:
+            block = torch.cat([block, block.new_zeros(rows - block.shape[0], d)])
+        v[i:i + rows] = ra.ra_mle_bind(help_ctx, block, False, r2)
+    assert tr["b_star"] == int(ra.ra_mle_bind(help_ctx, v.reshape(-1, 1), True, rho, field=True)[0])
